@@ -1,4 +1,4 @@
-"""ctypes binding of libvcas.so: one Python function per C entry point of include/vcas.h.
+"""ctypes binding of libvcas.so: one Python function per C entry point of include/vcas.h and include/vcas_train.h.
 
 Argument marshalling only: torch tensors provide device memory and the current CUDA stream,
 every step of the method runs in the library's kernels.  If the compiled library is missing
@@ -26,7 +26,11 @@ EXPORTS = ["vcas_default_config", "vcas_create", "vcas_destroy", "vcas_workspace
            "vcas_variance_probe", "vcas_update_ratios", "vcas_last_device_status", "vcas_launch_count",
            "vcas_set_profiling", "vcas_stage_times", "vcas_set_wait_limit",
            "vcas_set_probe_subsample", "vcas_get_probe_subsample", "vcas_score_static", "vcas_set_tuning",
-           "vcas_last_plan", "vcas_version"]
+           "vcas_last_plan", "vcas_version",
+           "vcas_loss_create", "vcas_loss_destroy", "vcas_loss_fwd", "vcas_loss_bwd", "vcas_loss_status",
+           "vcas_adamw_step", "vcas_adamw_rates",
+           "vcas_attn_create", "vcas_attn_destroy", "vcas_attn_workspace_bytes", "vcas_attn_fwd", "vcas_attn_bwd",
+           "vcas_attn_status", "vcas_attn_set_wait_limit"]
 
 
 class VcasError(RuntimeError):
@@ -56,7 +60,32 @@ class ChainArgs(C.Structure):
                 ("kept_cnt_out", C.c_void_p), ("skip_dropped_rows", C.c_int32), ("defer_join", C.c_int32)]
 
 
+class AttnDesc(C.Structure):
+    _fields_ = [("max_tokens", C.c_int32), ("max_seqs", C.c_int32), ("heads_q", C.c_int32), ("heads_kv", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32), ("causal", C.c_int32), ("scale", C.c_float)]
+
+
+class AttnTensor(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("token", C.c_int64), ("head", C.c_int64)]
+
+
+class LossDesc(C.Structure):
+    _fields_ = [("max_rows", C.c_int32), ("vocab", C.c_int32), ("dtype", C.c_int32), ("top", C.c_int32)]
+
+
+class AdamWEntry(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("g", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p),
+                ("v_scale", C.c_void_p), ("copy", C.c_void_p), ("n", C.c_int64), ("weight_decay", C.c_float),
+                ("p_dtype", C.c_int32), ("g_dtype", C.c_int32), ("state_bits", C.c_int32)]
+
+
+class AdamWArgs(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("step", C.c_int64),
+                ("seed", C.c_uint64), ("grad_scale", C.c_void_p), ("rates", C.c_void_p), ("seed_dev", C.c_void_p)]
+
+
 _P, _I, _F, _U64 = C.c_void_p, C.c_int32, C.c_float, C.c_uint64
+_I64, _D = C.c_int64, C.c_double
 # argument types, so that plain numbers and addresses can be passed (void pointers take an int or None)
 _SAMPLING_OUT = [_P] * 8
 ARGTYPES = {
@@ -77,6 +106,13 @@ ARGTYPES = {
     "vcas_set_probe_subsample": [_P, _I, _U64], "vcas_get_probe_subsample": [_P] * 3,
     "vcas_score_static": [_I] * 5 + [_P, _P, _F, _F, _U64] + _SAMPLING_OUT + [_P],
     "vcas_set_tuning": [_P] + [_I] * 6, "vcas_last_plan": [_P] * 2, "vcas_version": [],
+    "vcas_loss_create": [_P] * 2, "vcas_loss_destroy": [_P], "vcas_loss_status": [_P] * 2,
+    "vcas_loss_fwd": [_P, _P, _I64, _P, _I, _I] + [_P] * 6,
+    "vcas_loss_bwd": [_P, _P, _I64, _P, _I, _I] + [_P] * 5 + [_I64] + [_P] * 2,
+    "vcas_attn_create": [_P] * 2, "vcas_attn_destroy": [_P], "vcas_attn_workspace_bytes": [_P] * 2, "vcas_attn_status": [_P] * 2,
+    "vcas_attn_fwd": [_P] * 5 + [_I, _I] + [_P] * 3, "vcas_attn_set_wait_limit": [_P, _U64, _I],
+    "vcas_attn_bwd": [_P] * 8 + [_I, _I, _P, _P, _I] + [_P] * 4,
+    "vcas_adamw_step": [_P, _I, _P, _P], "vcas_adamw_rates": [_D, _D, _D, _I64, _P],
 }
 
 _lib = None
@@ -365,6 +401,284 @@ def score_static(X, dY, N: int, T: int, rho: float, nu: float, seed: int) -> Sam
                                  *_sampling_ptrs(b), _stream())
     _check(rc, "vcas_score_static")
     return Layer._pack_sampling(b)
+
+
+# --------------------------------------------------------------------- around the sampled backward (vcas_train.h)
+_DTYPES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _stream_of(device: torch.device):
+    return _raw_stream(device.index) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
+
+
+def _on(device, what: str, *tensors) -> None:
+    for t in tensors:
+        _need(t is None or t.device == device, f"{what} on {device} only")
+
+
+def _current_device() -> torch.device:
+    if not torch.cuda.is_available():
+        raise RuntimeError("libvcas needs a CUDA device (sm_100a); there is no CPU path")
+    return torch.device("cuda", torch.cuda.current_device())
+
+
+class _Handle:
+    """Creates a handle on the current device and destroys it with the object.  Calls are enqueued on that device's current
+    stream, whichever device is current."""
+    _kind = ""
+
+    def _create(self, desc) -> None:
+        self.device = _current_device()
+        self._h = C.c_void_p(None)
+        _check(getattr(lib(), f"vcas_{self._kind}_create")(C.byref(self._h), C.byref(desc)), f"vcas_{self._kind}_create")
+
+    def device_status(self) -> int:
+        st = C.c_int32(0)
+        _check(getattr(lib(), f"vcas_{self._kind}_status")(self._h, C.byref(st)), f"vcas_{self._kind}_status")
+        return st.value
+
+    def close(self) -> None:
+        if getattr(self, "_h", None) is not None and self._h.value:
+            getattr(lib(), f"vcas_{self._kind}_destroy")(self._h)
+            self._h = C.c_void_p(None)
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Attention(_Handle):
+    """Self-attention over packed sequences of up to max_tokens tokens in up to max_seqs sequences (vcas_attn_*).  Tensors are
+    [total, heads, head_dim] with any strides that keep a head's values side by side; starts: int32 [N + 1] on the device."""
+    _kind = "attn"
+
+    def __init__(self, max_tokens: int, max_seqs: int, heads_q: int, heads_kv: int, head_dim: int,
+                 dtype: torch.dtype = torch.bfloat16, causal: bool = False, scale: float = 0.0):
+        _need(dtype in _DTYPES, "attention is in bfloat16 or float32")
+        self.heads_q, self.heads_kv, self.head_dim, self.dtype = heads_q, heads_kv, head_dim, dtype
+        self._create(AttnDesc(max_tokens, max_seqs, heads_q, heads_kv, head_dim, _DTYPES[dtype], 1 if causal else 0, scale))
+
+    def _tensor(self, t, total: int, heads: int, written: bool = False) -> AttnTensor:
+        _need(t.shape == (total, heads, self.head_dim) and t.dtype == self.dtype,
+              f"expected [{total}, {heads}, {self.head_dim}] of {self.dtype}, got {tuple(t.shape)} of {t.dtype}")
+        _need(t.device == self.device, f"tensors of a call on {self.device} only")
+        token, head, inner = t.stride()
+        _need(inner == 1 or self.head_dim == 1, "a head's values lie side by side")
+        if written:      # no two elements in one place
+            a, b = sorted(((token, total), (head, heads)))
+            least = self.head_dim
+            for stride, n in (a, b):
+                _need(n <= 1 or stride >= least, "rows of an output overlap")
+                least = max(least, stride * n) if n > 1 else least
+        return AttnTensor(t.data_ptr(), token, head)
+
+    def _sequences(self, q, starts):
+        _need(starts.dim() == 1 and starts.numel() >= 1 and starts.dtype == torch.int32 and starts.is_contiguous(),
+              "starts is int32 [N + 1]")
+        _on(self.device, "starts", starts)
+        return q.shape[0], starts.numel() - 1
+
+    def _lse(self, lse, total):
+        _need(lse.shape == (self.heads_q, total) and lse.dtype == torch.float32 and lse.is_contiguous(),
+              "lse is float32 [heads_q, total]")
+        _on(self.device, "lse", lse)
+        return lse.data_ptr()
+
+    def fwd(self, q, k, v, starts, *, o=None, lse=None):
+        """Returns (o, lse)."""
+        total, N = self._sequences(q, starts)
+        if o is None:
+            o = torch.empty(total, self.heads_q, self.head_dim, dtype=self.dtype, device=self.device)
+        if lse is None:
+            lse = torch.empty(self.heads_q, total, dtype=torch.float32, device=self.device)
+        r, Hq, Hk = C.byref, self.heads_q, self.heads_kv
+        _check(lib().vcas_attn_fwd(self._h, r(self._tensor(q, total, Hq)), r(self._tensor(k, total, Hk)),
+                                   r(self._tensor(v, total, Hk)), starts.data_ptr(), N, total,
+                                   r(self._tensor(o, total, Hq, True)), self._lse(lse, total), _stream_of(self.device)),
+               "vcas_attn_fwd")
+        return o, lse
+
+    def bwd(self, d_o, q, k, v, o, lse, starts, *, dq=None, dk=None, dv=None, alive_in=None, alive_cnt_in=None,
+            skip_dropped_rows: bool = False):
+        """Returns (dq, dk, dv).  alive_in, alive_cnt_in: the kept_out, kept_cnt_out of the layer above."""
+        total, N = self._sequences(q, starts)
+        Hq, Hk, D = self.heads_q, self.heads_kv, self.head_dim
+        new = lambda h: torch.empty(total, h, D, dtype=self.dtype, device=self.device)
+        dq, dk, dv = new(Hq) if dq is None else dq, new(Hk) if dk is None else dk, new(Hk) if dv is None else dv
+        _need((alive_in is None) == (alive_cnt_in is None), "alive_in and alive_cnt_in come together")
+        if alive_in is not None:
+            _need(alive_in.dtype == alive_cnt_in.dtype == torch.int32 and alive_in.numel() >= N and alive_cnt_in.numel() >= 1
+                  and alive_in.is_contiguous(), "alive_in is int32 [N], alive_cnt_in int32 [1]")
+            _on(self.device, "alive_in", alive_in, alive_cnt_in)
+        r, dp = C.byref, lambda t: None if t is None else t.data_ptr()
+        T = self._tensor
+        _check(lib().vcas_attn_bwd(self._h, r(T(d_o, total, Hq)), r(T(q, total, Hq)), r(T(k, total, Hk)), r(T(v, total, Hk)),
+                                   r(T(o, total, Hq)), self._lse(lse, total), starts.data_ptr(), N, total, dp(alive_in),
+                                   dp(alive_cnt_in), 1 if skip_dropped_rows else 0, r(T(dq, total, Hq, True)),
+                                   r(T(dk, total, Hk, True)), r(T(dv, total, Hk, True)), _stream_of(self.device)), "vcas_attn_bwd")
+        return dq, dk, dv
+
+    def set_wait_limit(self, limit_ns: int, stall_once: bool = False) -> None:
+        _check(lib().vcas_attn_set_wait_limit(self._h, limit_ns, 1 if stall_once else 0), "vcas_attn_set_wait_limit")
+
+    def workspace_bytes(self) -> int:
+        n = C.c_size_t(0)
+        _check(lib().vcas_attn_workspace_bytes(self._h, C.byref(n)), "vcas_attn_workspace_bytes")
+        return n.value
+
+
+@dataclass
+class LogProbs:
+    logp: torch.Tensor
+    entropy: torch.Tensor
+    lse: torch.Tensor
+    top_logp: torch.Tensor | None
+    top_ids: torch.Tensor | None
+
+
+class TokenLoss(_Handle):
+    """Log probabilities of given tokens, entropy and top alternatives of up to max_rows rows of `vocab` logits, and their
+    gradient (vcas_loss_*)."""
+    _kind = "loss"
+
+    def __init__(self, max_rows: int, vocab: int, dtype: torch.dtype = torch.bfloat16, top: int = 0):
+        _need(dtype in _DTYPES, "logits are bfloat16 or float32")
+        self.max_rows, self.vocab, self.dtype, self.top = max_rows, vocab, dtype, top
+        self._create(LossDesc(max_rows, vocab, _DTYPES[dtype], top))
+
+    def _rows(self, logits, tokens):
+        _need(logits.dim() == 2 and logits.shape[1] == self.vocab and logits.dtype == self.dtype,
+              f"logits are [rows, {self.vocab}] of {self.dtype}")
+        _need(logits.stride(1) == 1 or self.vocab == 1, "a row's logits lie side by side")
+        rows = logits.shape[0]
+        _need(rows <= 1 or logits.stride(0) >= self.vocab, "rows that overlap")
+        _need(tokens.shape == (rows,) and tokens.is_contiguous() and tokens.dtype in (torch.int32, torch.int64),
+              "tokens are [rows], int32 or int64")
+        _on(self.device, "logits and tokens", logits, tokens)
+        return rows, max(logits.stride(0), self.vocab)
+
+    def fwd(self, logits, tokens) -> LogProbs:
+        """tokens: [rows], negative where there is none."""
+        rows, ld = self._rows(logits, tokens)
+        f = torch.empty(3, rows, dtype=torch.float32, device=self.device)
+        tl = torch.empty(rows, self.top, dtype=torch.float32, device=self.device) if self.top else None
+        ti = torch.empty(rows, self.top, dtype=torch.int32, device=self.device) if self.top else None
+        base = f.data_ptr()
+        _check(lib().vcas_loss_fwd(self._h, logits.data_ptr(), ld, tokens.data_ptr(), tokens.element_size(), rows, base,
+                                   base + 4 * rows, base + 8 * rows, None if tl is None else tl.data_ptr(),
+                                   None if ti is None else ti.data_ptr(), _stream_of(self.device)), "vcas_loss_fwd")
+        return LogProbs(f[0], f[1], f[2], tl, ti)
+
+    def bwd(self, logits, tokens, lse, g_logp, *, entropy=None, g_entropy=None, dlogits=None, a_out=None):
+        """Returns (dlogits, a_out); dlogits may be logits itself.  a_out: the rows' square-norms for linear_bwd_chain(a_in=)."""
+        rows, ld = self._rows(logits, tokens)
+        vectors = [lse, g_logp] + [t for t in (entropy, g_entropy, a_out) if t is not None]
+        _need(all(t.shape == (rows,) and t.dtype == torch.float32 and t.is_contiguous() for t in vectors),
+              "lse, entropy and the derivatives are [rows] of float32")
+        if dlogits is None:
+            dlogits = torch.empty(rows, self.vocab, dtype=self.dtype, device=self.device)
+        if a_out is None:
+            a_out = torch.empty(rows, dtype=torch.float32, device=self.device)
+        _, ld_d = self._rows(dlogits, tokens)
+        _on(self.device, "lse, entropy and the derivatives", a_out, *vectors)
+        dp = lambda t: None if t is None else t.data_ptr()
+        _check(lib().vcas_loss_bwd(self._h, logits.data_ptr(), ld, tokens.data_ptr(), tokens.element_size(), rows, dp(lse),
+                                   dp(entropy), dp(g_logp), dp(g_entropy), dp(dlogits), ld_d, dp(a_out),
+                                   _stream_of(self.device)), "vcas_loss_bwd")
+        return dlogits, a_out
+
+
+@dataclass
+class AdamWTensor:
+    """One tensor of an AdamW step.  m, v: float32, or float8_e4m3fn (v then holds sqrt(v)) with m_scale and v_scale, one float32
+    for each 256 elements.  copy: bfloat16 copy of p to be written (float32 p)."""
+    p: torch.Tensor
+    g: torch.Tensor
+    m: torch.Tensor
+    v: torch.Tensor
+    m_scale: torch.Tensor | None = None
+    v_scale: torch.Tensor | None = None
+    copy: torch.Tensor | None = None
+    weight_decay: float = 0.0
+
+    @staticmethod
+    def make(p, g, bits: int = 32, copy=None, weight_decay: float = 0.0) -> "AdamWTensor":
+        """With fresh states of 32 or 8 bits."""
+        z = lambda n, dt: torch.zeros(n, dtype=dt, device=p.device)
+        if bits == 32:
+            return AdamWTensor(p, g, z(p.shape, torch.float32), z(p.shape, torch.float32), copy=copy, weight_decay=weight_decay)
+        n = (p.numel() + 255) // 256
+        e4m3 = lambda: torch.zeros(p.shape, dtype=torch.uint8, device=p.device).view(torch.float8_e4m3fn)
+        return AdamWTensor(p, g, e4m3(), e4m3(), z(n, torch.float32), z(n, torch.float32), copy, weight_decay)
+
+
+class AdamW:
+    """AdamW over a list of tensors in one launch for each combination of types (vcas_adamw_step).  Holds the tensors; `g` of an
+    entry may be set between steps with set_grad."""
+
+    def __init__(self, tensors: list[AdamWTensor]):
+        self.device = tensors[0].p.device if tensors else _current_device()
+        self.tensors = list(tensors)
+        self._table = (AdamWEntry * max(1, len(tensors)))()
+        for i, t in enumerate(self.tensors):
+            self._fill(i, t)
+
+    def _fill(self, i: int, t: AdamWTensor) -> None:
+        bits = 8 if t.m.dtype == torch.float8_e4m3fn else 32
+        n = t.p.numel()
+        _need(t.p.dtype in _DTYPES, "p is float32 or bfloat16")
+        _need(t.m.dtype == t.v.dtype and t.m.dtype in (torch.float32, torch.float8_e4m3fn), "states are float32 or float8_e4m3fn")
+        _need(t.m.numel() == n and t.v.numel() == n, "states have an element for each of p")
+        scales = [t.m_scale, t.v_scale]
+        if bits == 8:
+            _need(all(s is not None and s.dtype == torch.float32 and s.numel() == (n + 255) // 256 for s in scales),
+                  "8-bit states have a float32 scale for each 256 elements")
+        else:
+            _need(scales == [None, None], "float32 states have no scales")
+        _need(t.copy is None or (t.copy.dtype == torch.bfloat16 and t.copy.numel() == n and t.p.dtype == torch.float32),
+              "copy is bfloat16, of a float32 p")
+        every = [x for x in (t.p, t.m, t.v, t.m_scale, t.v_scale, t.copy) if x is not None]
+        _need(all(x.is_cuda and x.is_contiguous() for x in every), "device-resident contiguous tensors only")
+        _on(self.device, "tensors of a step", *every)
+        dp = lambda x: None if x is None else x.data_ptr()
+        self._table[i] = AdamWEntry(dp(t.p), None, dp(t.m), dp(t.v), dp(t.m_scale), dp(t.v_scale), dp(t.copy), n, t.weight_decay,
+                                    _DTYPES[t.p.dtype], 0, bits)
+        self.set_grad(i, t.g)
+
+    def set_grad(self, i: int, g: torch.Tensor) -> None:
+        t = self.tensors[i]
+        _need(g.dtype in _DTYPES and g.numel() == t.p.numel() and g.is_contiguous(), "g is contiguous, float32 or bfloat16, as large as p")
+        _on(self.device, "gradients of a step", g)
+        t.g = g
+        self._table[i].g, self._table[i].g_dtype = g.data_ptr(), _DTYPES[g.dtype]
+
+    def step(self, step: int, *, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, seed: int = 0,
+             grad_scale=None, rates=None, seed_dev=None) -> None:
+        """step: 1 for the first.  seed: another one each step (8-bit states).  grad_scale: float32 [1] on the device.
+        rates (adamw_rates, float32 [3]) and seed_dev (int64 [1]) on the device are read in place of lr and step, and of seed:
+        a captured step then follows them."""
+        ok = lambda t, n, dt: t is None or (t.dtype == dt and t.numel() == n and t.is_contiguous())
+        _need(ok(grad_scale, 1, torch.float32) and ok(rates, 3, torch.float32) and ok(seed_dev, 1, torch.int64),
+              "grad_scale is float32 [1], rates float32 [3], seed_dev int64 [1]")
+        _on(self.device, "grad_scale, rates and seed_dev", grad_scale, rates, seed_dev)
+        dp = lambda t: None if t is None else t.data_ptr()
+        args = AdamWArgs(lr, beta1, beta2, eps, step, seed & 0xFFFFFFFFFFFFFFFF, dp(grad_scale), dp(rates), dp(seed_dev))
+        with torch.cuda.device(self.device):
+            _check(lib().vcas_adamw_step(self._table, len(self.tensors), C.byref(args), _stream_of(self.device)), "vcas_adamw_step")
+
+
+def adamw_rates(lr: float, beta1: float, beta2: float, step: int) -> torch.Tensor:
+    """float32 [3] on the host: what AdamW.step(rates=) reads, once copied to the device."""
+    r = (C.c_float * 3)()
+    _check(lib().vcas_adamw_rates(lr, beta1, beta2, step, r), "vcas_adamw_rates")
+    return torch.tensor(list(r), dtype=torch.float32)
 
 
 def version() -> int:

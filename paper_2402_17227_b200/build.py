@@ -9,14 +9,14 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libvcas.so")
-SOURCES = ["api.cu", "score.cu", "sampler.cu", "gemm_fma.cu", "gemm_umma.cu", "gemm_split.cu", "probe.cu", "probe_fused.cu", "score_static.cu", "layernorm.cu"]
+SOURCES = ["api.cu", "score.cu", "sampler.cu", "gemm_fma.cu", "gemm_umma.cu", "gemm_split.cu", "probe.cu", "probe_fused.cu", "score_static.cu", "layernorm.cu", "adamw.cu", "loss.cu", "attn.cu", "attn_umma.cu"]
 
 
 def _stale() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(ROOT, "include", "vcas.h")]
+    deps = [os.path.join(d, f) for d in (CSRC, os.path.join(ROOT, "include")) for f in os.listdir(d)]
     return any(os.path.getmtime(d) > t for d in deps)
 
 

@@ -1,0 +1,348 @@
+// AdamW over many tensors in one launch (vcas_adamw_step).
+//
+// HBM-bound: a thread takes eight consecutive elements, every array is read and written once with the widest access there is (32
+// bytes of fp32, 16 of bf16, 8 of e4m3), and the whole table of tensors travels in the kernel's parameters, so that a step
+// neither copies a table to the device nor keeps one there.  A warp's 256 elements are the block of an 8-bit state's scale: its
+// largest value is one warp reduction, on the bits as integers, which carry a NaN along.
+// Every multiplication and addition is rounded on its own (no contraction to fma): the update is then the same to
+// the bit wherever it is computed from the formulas.
+#include <cmath>
+
+#include "common.cuh"
+#include "vcas_train.h"
+
+namespace vcas {
+namespace {
+
+constexpr int THREADS = 256;
+constexpr int CHUNK = THREADS * 8;       // elements a CTA works on
+
+struct Entry {
+  void* p; const void* g; void* m; void* v; float* m_scale; float* v_scale; void* copy;
+  int64_t n;
+  float keep, decay;                     // 1 - lr wd, wd
+  uint32_t first;                        // first chunk of this tensor in the launch
+  uint32_t place;                        // in the caller's list, and in the top bit whether all pointers are aligned
+};
+// Kernel parameters hold 32 KB; most lists are short, and a small table is launched faster.
+constexpr int SMALL = 48, LARGE = 384;
+template <int CAP>
+struct Table {
+  Entry e[CAP];
+  int count;
+  float b1, c1, b2, c2, eps, step_size, inv;
+  uint32_t seed_lo, seed_hi;
+  const float* grad_scale; const float* rates; const uint64_t* seed_dev;
+};
+static_assert(sizeof(Table<LARGE>) <= 32764, "kernel parameters");
+
+// ---- eight consecutive elements
+__device__ __forceinline__ void ld8(const float* p, float (&f)[8]) {
+  asm volatile("ld.global.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=f"(f[0]), "=f"(f[1]), "=f"(f[2]), "=f"(f[3]), "=f"(f[4]), "=f"(f[5]), "=f"(f[6]), "=f"(f[7]) : "l"(p) : "memory");
+}
+__device__ __forceinline__ void st8(float* p, const float (&f)[8]) {
+  asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+               ::"l"(p), "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7]) : "memory");
+}
+__device__ __forceinline__ void ld8(const __nv_bfloat16* p, float (&f)[8]) {
+  const uint4 v = *reinterpret_cast<const uint4*>(p);
+  const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(u[i] << 16); f[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
+}
+__device__ __forceinline__ void st8(__nv_bfloat16* p, const float (&f)[8]) {
+  uint32_t u[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 t = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+    u[i] = *reinterpret_cast<const uint32_t*>(&t);
+  }
+  *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+}
+__device__ __forceinline__ float widen(float x) { return x; }
+__device__ __forceinline__ float widen(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ void narrow(float x, float* p) { *p = x; }
+__device__ __forceinline__ void narrow(float x, __nv_bfloat16* p) { *p = __float2bfloat16_rn(x); }
+
+// the group's first `have` elements; the others count as zeros
+template <typename T>
+__device__ __forceinline__ void load(const T* p, int have, bool wide, float (&f)[8]) {
+  if (wide) { ld8(p, f); return; }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = i < have ? widen(p[i]) : 0.f;
+}
+template <typename T>
+__device__ __forceinline__ void store(T* p, int have, bool wide, const float (&f)[8]) {
+  if (wide) { st8(p, f); return; }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i < have) narrow(f[i], p + i);
+}
+__device__ __forceinline__ uint2 load_codes(const uint8_t* p, int have, bool wide) {
+  if (wide) return *reinterpret_cast<const uint2*>(p);
+  uint32_t w[2] = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i < have) w[i / 4] |= (uint32_t)p[i] << (8 * (i % 4));
+  return make_uint2(w[0], w[1]);
+}
+__device__ __forceinline__ void store_codes(uint8_t* p, int have, bool wide, uint2 c) {
+  if (wide) { *reinterpret_cast<uint2*>(p) = c; return; }
+  const uint32_t w[2] = {c.x, c.y};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i < have) p[i] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
+}
+
+// ---- e4m3: sign, four exponent bits, three of the mantissa.  Times 2^120 its exponent and mantissa are bits 20-26 of an fp32
+// value, subnormals included.
+__device__ __forceinline__ void decode(uint2 c, float scale, float (&f)[8]) {
+  const float up = 0x1p+120f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t b = (i < 4 ? c.x : c.y) >> (8 * (i % 4));
+    // code * 2^120 is exact, so this is the value itself, rounded once with the scale
+    f[i] = __fmul_rn(__fmul_rn(__uint_as_float(((b & 0x7fu) << 20) | ((b & 0x80u) << 24)), up), scale);
+  }
+}
+// LEAST: 1 where a positive value must not become 0
+template <uint32_t LEAST, int SHIFT>
+__device__ __forceinline__ uint2 encode(const float (&f)[8], const uint32_t (&rnd)[4], float* scale_at, int lane) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
+  const float big = __uint_as_float(__reduce_max_sync(0xffffffffu, top));
+  if (lane == 0) *scale_at = __fmul_rn(big, 1.0f / 448.0f);
+  // under 2^-100 (sqrt(v) is never that small) 448 / big would leave fp32's range: such an m is held as 0
+  const float inv = big >= 0x1p-100f ? __fdiv_rn(448.0f, big) : 0.f;
+  uint32_t w[2] = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float y = fminf(__fmul_rn(fabsf(f[i]), inv), 448.0f);
+    const uint32_t r = (rnd[i / 2] >> (16 * (i % 2) + SHIFT)) & 0xffu;
+    uint32_t c = (__float_as_uint(__fmul_rn(y, 0x1p-120f)) + (r << 12) + 2048u) >> 20;
+    if (LEAST) c = f[i] > 0.f ? max(c, LEAST) : c;
+    else c |= f[i] < 0.f ? 0x80u : 0u;
+    w[i / 4] |= c << (8 * (i % 4));
+  }
+  return make_uint2(w[0], w[1]);
+}
+
+__device__ __forceinline__ void philox(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t k0, uint32_t k1, uint32_t (&out)[4]) {
+  uint32_t c3 = 0;
+#pragma unroll
+  for (int r = 0; r < 10; ++r) {
+    const uint32_t hi0 = __umulhi(0xD2511F53u, c0), lo0 = 0xD2511F53u * c0;
+    const uint32_t hi1 = __umulhi(0xCD9E8D57u, c2), lo1 = 0xCD9E8D57u * c2;
+    c0 = hi1 ^ c1 ^ k0; c1 = lo1; c2 = hi0 ^ c3 ^ k1; c3 = lo0;
+    k0 += 0x9E3779B9u; k1 += 0xBB67AE85u;
+  }
+  out[0] = c0; out[1] = c1; out[2] = c2; out[3] = c3;
+}
+
+template <typename P, typename G, int BITS, int CAP>
+__global__ void __launch_bounds__(THREADS) adamw_kernel(const __grid_constant__ Table<CAP> t) {
+  // the tensor this chunk belongs to: the last one that begins at or before it
+  int lo = 0, hi = t.count - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (t.e[mid].first <= blockIdx.x) lo = mid; else hi = mid - 1;
+  }
+  const Entry& e = t.e[lo];
+  const int64_t at = (int64_t)(blockIdx.x - e.first) * CHUNK + threadIdx.x * 8;
+  const int64_t left = e.n - at;
+  const int have = left >= 8 ? 8 : left > 0 ? (int)left : 0;
+  // a whole warp without elements has nothing to do; the others keep all lanes for the block's largest value
+  if (__all_sync(0xffffffffu, have == 0)) return;
+  const bool wide = have == 8 && (e.place >> 31);
+  const int lane = threadIdx.x & 31;
+
+  float p[8], g[8], m[8], v[8];
+  uint2 mc = make_uint2(0, 0), vc = make_uint2(0, 0);
+  float ms = 0.f, vs = 0.f;
+  const int64_t block = at >> 8;
+  load((const G*)e.g + at, have, wide, g);
+  if (BITS == 32) {
+    load((const float*)e.m + at, have, wide, m);
+    load((const float*)e.v + at, have, wide, v);
+  } else {
+    mc = load_codes((const uint8_t*)e.m + at, have, wide);
+    vc = load_codes((const uint8_t*)e.v + at, have, wide);
+    ms = e.m_scale[block];
+    vs = e.v_scale[block];
+  }
+  load((const P*)e.p + at, have, wide, p);
+  float keep = e.keep, step_size = t.step_size, inv = t.inv;
+  if (t.rates != nullptr) {
+    keep = (float)(1.0 - (double)t.rates[0] * (double)e.decay);
+    step_size = t.rates[1];
+    inv = t.rates[2];
+  }
+  if (t.grad_scale != nullptr) {
+    const float s = *t.grad_scale;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) g[i] = __fmul_rn(g[i], s);
+  }
+  if (BITS == 8) {
+    decode(mc, ms, m);
+    decode(vc, vs, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], v[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    m[i] = __fadd_rn(__fmul_rn(m[i], t.b1), __fmul_rn(g[i], t.c1));
+    v[i] = __fadd_rn(__fmul_rn(v[i], t.b2), __fmul_rn(__fmul_rn(g[i], g[i]), t.c2));
+    const float root = __fsqrt_rn(v[i]);
+    const float denom = __fadd_rn(__fmul_rn(root, inv), t.eps);
+    p[i] = __fadd_rn(__fmul_rn(p[i], keep), -__fdiv_rn(__fmul_rn(m[i], step_size), denom));
+    if (BITS == 8) v[i] = root;
+  }
+  store((P*)e.p + at, have, wide, p);
+  if (sizeof(P) == 4 && e.copy != nullptr) store((__nv_bfloat16*)e.copy + at, have, wide, p);
+  if (BITS == 32) {
+    store((float*)e.m + at, have, wide, m);
+    store((float*)e.v + at, have, wide, v);
+  } else {
+    // elements behind the tensor's end count as zeros (0 / (0 + eps) leaves m and r at 0)
+    uint32_t k0 = t.seed_lo, k1 = t.seed_hi, rnd[4];
+    if (t.seed_dev != nullptr) { const uint64_t s = *t.seed_dev; k0 = (uint32_t)s; k1 = (uint32_t)(s >> 32); }
+    philox((uint32_t)(at >> 3), e.place & 0x7fffffffu, 3u, k0, k1, rnd);
+    const uint2 mo = encode<0, 0>(m, rnd, e.m_scale + block, lane);
+    const uint2 vo = encode<1, 8>(v, rnd, e.v_scale + block, lane);
+    store_codes((uint8_t*)e.m + at, have, wide, mo);
+    store_codes((uint8_t*)e.v + at, have, wide, vo);
+  }
+}
+
+bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+
+template <typename P, typename G, int BITS, int CAP>
+cudaError_t launch(const Table<CAP>& t, uint32_t chunks, cudaStream_t st) {
+  adamw_kernel<P, G, BITS, CAP><<<chunks, THREADS, 0, st>>>(t);
+  return cudaGetLastError();
+}
+template <int CAP>
+cudaError_t launch_class(int cls, const Table<CAP>& t, uint32_t chunks, cudaStream_t st) {
+  using B = __nv_bfloat16;
+  switch (cls) {
+    case 0: return launch<float, float, 32, CAP>(t, chunks, st);
+    case 1: return launch<B, float, 32, CAP>(t, chunks, st);
+    case 2: return launch<float, B, 32, CAP>(t, chunks, st);
+    case 3: return launch<B, B, 32, CAP>(t, chunks, st);
+    case 4: return launch<float, float, 8, CAP>(t, chunks, st);
+    case 5: return launch<B, float, 8, CAP>(t, chunks, st);
+    case 6: return launch<float, B, 8, CAP>(t, chunks, st);
+    default: return launch<B, B, 8, CAP>(t, chunks, st);
+  }
+}
+
+int class_of(const vcas_adamw_tensor& x) {
+  return (x.p_dtype == VCAS_DTYPE_BF16 ? 1 : 0) + (x.g_dtype == VCAS_DTYPE_BF16 ? 2 : 0) + (x.state_bits == 8 ? 4 : 0);
+}
+
+// The next launch of one class: tensors from `from` on, at most CAP of them and 2^30 chunks.
+template <int CAP>
+int fill(const vcas_adamw_tensor* ts, int n, int cls, int from, double lr, Table<CAP>& t, uint32_t* chunks) {
+  t.count = 0;
+  *chunks = 0;
+  int i = from;
+  for (; i < n && t.count < CAP; ++i) {
+    const vcas_adamw_tensor& x = ts[i];
+    if (x.n == 0 || class_of(x) != cls) continue;
+    const int64_t c = (x.n + CHUNK - 1) / CHUNK;
+    if (*chunks + c > (1u << 30)) break;
+    Entry& e = t.e[t.count++];
+    e.p = x.p; e.g = x.g; e.m = x.m; e.v = x.v; e.m_scale = x.m_scale; e.v_scale = x.v_scale; e.copy = x.copy;
+    e.n = x.n;
+    e.keep = (float)(1.0 - lr * (double)x.weight_decay);
+    e.decay = x.weight_decay;
+    e.first = *chunks;
+    const size_t pa = x.p_dtype == VCAS_DTYPE_BF16 ? 16 : 32, ga = x.g_dtype == VCAS_DTYPE_BF16 ? 16 : 32;
+    const size_t sa = x.state_bits == 8 ? 8 : 32;
+    const bool wide = aligned(x.p, pa) && aligned(x.g, ga) && aligned(x.m, sa) && aligned(x.v, sa) && aligned(x.copy, 16);
+    e.place = (uint32_t)i | (wide ? 0x80000000u : 0u);
+    *chunks += (uint32_t)c;
+  }
+  return i;
+}
+
+template <int CAP>
+cudaError_t run(const vcas_adamw_tensor* ts, int n, int cls, const vcas_adamw_args& a, cudaStream_t st) {
+  Table<CAP> t;
+  t.b1 = (float)a.beta1; t.c1 = (float)(1.0 - a.beta1);
+  t.b2 = (float)a.beta2; t.c2 = (float)(1.0 - a.beta2);
+  t.eps = (float)a.eps;
+  t.step_size = t.inv = 0.f;
+  double lr = a.lr;
+  if (a.rates == nullptr) {
+    float r[3];
+    vcas_adamw_rates(a.lr, a.beta1, a.beta2, a.step, r);
+    t.step_size = r[1];
+    t.inv = r[2];
+  } else {
+    lr = 0.0;
+  }
+  t.seed_lo = (uint32_t)a.seed; t.seed_hi = (uint32_t)(a.seed >> 32);
+  t.grad_scale = a.grad_scale; t.rates = a.rates; t.seed_dev = a.seed_dev;
+  for (int from = 0; from < n;) {
+    uint32_t chunks = 0;
+    from = fill<CAP>(ts, n, cls, from, lr, t, &chunks);
+    if (t.count == 0) continue;
+    const cudaError_t e = launch_class<CAP>(cls, t, chunks, st);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+bool in_unit(double b) { return b >= 0.0 && b < 1.0; }
+
+}  // namespace
+}  // namespace vcas
+
+using namespace vcas;
+
+extern "C" int vcas_adamw_rates(double lr, double beta1, double beta2, int64_t step, float* rates) {
+  if (rates == nullptr || !std::isfinite(lr) || lr < 0.0 || !in_unit(beta1) || !in_unit(beta2) || step < 1) return VCAS_ERR_BAD_ARG;
+  rates[0] = (float)lr;
+  rates[1] = (float)(lr / (1.0 - std::pow(beta1, (double)step)));
+  rates[2] = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
+  return VCAS_OK;
+}
+
+extern "C" int vcas_adamw_step(const vcas_adamw_tensor* ts, int32_t n, const vcas_adamw_args* args, vcas_stream stream) {
+  if (n < 0 || args == nullptr || (n > 0 && ts == nullptr)) return VCAS_ERR_BAD_ARG;
+  float unused[3];
+  const vcas_adamw_args& a = *args;
+  const int rc = vcas_adamw_rates(a.rates == nullptr ? a.lr : 0.0, a.beta1, a.beta2, a.rates == nullptr ? a.step : 1, unused);
+  if (rc != VCAS_OK) return rc;
+  if (!std::isfinite(a.eps) || a.eps < 0.0) return VCAS_ERR_BAD_ARG;
+  int in_class[8] = {};
+  for (int i = 0; i < n; ++i) {
+    const vcas_adamw_tensor& x = ts[i];
+    if (x.n < 0 || x.n > (int64_t)1 << 34) return VCAS_ERR_SHAPE;
+    if ((x.p_dtype != VCAS_DTYPE_F32 && x.p_dtype != VCAS_DTYPE_BF16) ||
+        (x.g_dtype != VCAS_DTYPE_F32 && x.g_dtype != VCAS_DTYPE_BF16) || (x.state_bits != 8 && x.state_bits != 32))
+      return VCAS_ERR_DTYPE;
+    if (!std::isfinite(x.weight_decay) || x.weight_decay < 0.f) return VCAS_ERR_BAD_ARG;
+    if (x.copy != nullptr && x.p_dtype != VCAS_DTYPE_F32) return VCAS_ERR_DTYPE;
+    if (x.n == 0) continue;
+    if (x.p == nullptr || x.g == nullptr || x.m == nullptr || x.v == nullptr ||
+        (x.state_bits == 8 && (x.m_scale == nullptr || x.v_scale == nullptr)))
+      return VCAS_ERR_BAD_ARG;
+    const size_t pa = x.p_dtype == VCAS_DTYPE_BF16 ? 2 : 4, ga = x.g_dtype == VCAS_DTYPE_BF16 ? 2 : 4;
+    const size_t sa = x.state_bits == 8 ? 1 : 4;
+    if (!aligned(x.p, pa) || !aligned(x.g, ga) || !aligned(x.m, sa) || !aligned(x.v, sa) || !aligned(x.copy, 2) ||
+        !aligned(x.m_scale, 4) || !aligned(x.v_scale, 4))
+      return VCAS_ERR_BAD_ARG;
+    ++in_class[class_of(x)];
+  }
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  for (int c = 0; c < 8; ++c) {
+    if (in_class[c] == 0) continue;
+    const cudaError_t e = in_class[c] <= SMALL ? run<SMALL>(ts, n, c, a, st) : run<LARGE>(ts, n, c, a, st);
+    if (e != cudaSuccess) return VCAS_ERR_CUDA;
+  }
+  return VCAS_OK;
+}

@@ -1,0 +1,114 @@
+// What the attention kernels share: the handle, the tensors of a call, and how a CTA finds its part of a packed sequence.
+#pragma once
+
+#include "common.cuh"
+#include "vcas_train.h"
+
+namespace vcas {
+
+struct Attn {
+  vcas_attn_desc desc;
+  int device, num_sms;
+  float scale;
+  bool tensor_ok;        // bf16 on a device with tcgen05
+  void* base;
+  size_t bytes;
+  float* delta;          // [heads_q][max_tokens] rowsum(dO O)
+  int32_t* status;
+  unsigned long long wait_limit_ns;
+  int stall_once;
+};
+
+// The sequences of a call.  alive (with its length): the only ones that are worked on.
+struct Seqs {
+  const int32_t* starts;
+  const int32_t* alive; const int32_t* alive_cnt;
+  int N, total;
+  int32_t* status;
+};
+
+struct Strided { const void* p; int64_t token, head; };
+
+struct AttnCall {
+  Seqs seqs;
+  Strided q, k, v, o, d_o, dq, dk, dv;       // o is written by the forward, dq, dk and dv by the backward
+  float* lse;                                // [heads_q][total]
+  float* delta;                              // [heads_q][total]
+  int heads_q, heads_kv, group, dim, causal;
+  float scale;
+  int skip_dropped;
+};
+
+constexpr float ATTN_LOG2E = 1.4426950408889634f, ATTN_LN2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float attn_exp2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Sequence n: its first token and length; 0 tokens and a note in the status word where starts make no sense there.
+__device__ __forceinline__ int seq_length(const Seqs& q, int n, int& first) {
+  const int s = q.starts[n], e = q.starts[n + 1];
+  first = s;
+  if (s < 0 || e < s || e > q.total) {
+    atomicExch(q.status, (int32_t)VCAS_ERR_BAD_ARG);
+    return 0;
+  }
+  return e - s;
+}
+__device__ __forceinline__ int seq_count(const Seqs& q) {
+  if (q.alive == nullptr) return q.N;
+  const int c = *q.alive_cnt;
+  if (c >= 0 && c <= q.N) return c;
+  atomicExch(q.status, (int32_t)VCAS_ERR_BAD_ARG);
+  return 0;
+}
+
+// Tile number `tile` of all sequences cut into tiles of `rows` tokens, sequence by sequence: its sequence's first token and length, and
+// its place in the sequence.  By one full warp, 32 sequences at a time; false where there are not that many tiles.
+__device__ __forceinline__ bool find_tile(const Seqs& q, int tile, int rows, int lane, int& first, int& len, int& place) {
+  const int count = seq_count(q);
+  int before = 0;
+  for (int b = 0; b < count; b += 32) {
+    int n = b + lane < count ? b + lane : -1, s = 0, l = 0;
+    if (n >= 0 && q.alive != nullptr) {
+      n = q.alive[n];
+      if (n < 0 || n >= q.N) {
+        atomicExch(q.status, (int32_t)VCAS_ERR_BAD_ARG);
+        n = -1;
+      }
+    }
+    if (n >= 0) l = seq_length(q, n, s);
+    const int tiles = (l + rows - 1) / rows;
+    int upto = tiles;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += v;
+    }
+    const unsigned hit = __ballot_sync(0xffffffffu, tile < before + upto);
+    if (hit != 0) {
+      const int at = __ffs(hit) - 1;
+      first = __shfl_sync(0xffffffffu, s, at);
+      len = __shfl_sync(0xffffffffu, l, at);
+      place = tile - before - __shfl_sync(0xffffffffu, upto - tiles, at);
+      return true;
+    }
+    before += __shfl_sync(0xffffffffu, upto, 31);
+  }
+  return false;
+}
+
+// No more tiles than these exist where sequences do not overlap: a sequence adds one that is not full at most.
+inline long tile_bound(int total, int N, int rows) { return total / rows + (N < total ? N : total); }
+
+cudaError_t launch_attn_fma_fwd(const Attn* a, const AttnCall& c, cudaStream_t st);
+cudaError_t launch_attn_fma_bwd(const Attn* a, const AttnCall& c, cudaStream_t st);
+// delta = rowsum(dO O) on the rows of the sequences that are worked on, zeros into dq, dk, dv on those of the others
+cudaError_t launch_attn_rows(const Attn* a, const AttnCall& c, cudaStream_t st);
+bool attn_umma_ok(const Attn* a, const AttnCall& c, bool backward);
+cudaError_t launch_attn_umma_fwd(const Attn* a, const AttnCall& c, cudaStream_t st);
+cudaError_t launch_attn_umma_bwd(const Attn* a, const AttnCall& c, cudaStream_t st);
+
+}  // namespace vcas

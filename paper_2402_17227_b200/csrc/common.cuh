@@ -207,6 +207,21 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   return d;
 }
 
+// Makes a handle's device the current one for the length of a call.
+struct DeviceScope {
+  int before = -1;
+  bool ok;
+  explicit DeviceScope(int device) {
+    ok = cudaGetDevice(&before) == cudaSuccess && (before == device || cudaSetDevice(device) == cudaSuccess);
+    if (before == device) before = -1;
+  }
+  ~DeviceScope() {
+    if (before >= 0) cudaSetDevice(before);
+  }
+  DeviceScope(const DeviceScope&) = delete;
+  DeviceScope& operator=(const DeviceScope&) = delete;
+};
+
 // ---------------------------------------------------------------------------------------
 // SampleA inside one warp (Sec. 4.1), shared by the sampling kernel and the tail of the row-norm kernel.
 // ---------------------------------------------------------------------------------------
