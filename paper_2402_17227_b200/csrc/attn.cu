@@ -286,9 +286,11 @@ __global__ void __launch_bounds__(THREADS) attn_fma_dkv_kernel(AttnCall C) {
   store_rows<T, DP>(C.dk, p.first, p.len, p.t0, p.head, C.dim, tx, ty, dk, f);
 }
 
-// A warp per token: delta of its heads if its sequence is worked on, else zeros in its rows of the gradients.
-template <typename T>
-__global__ void __launch_bounds__(256) attn_rows_kernel(AttnCall C) {
+// A warp per token: delta of its heads if its sequence is worked on (DELTA), else zeros in its rows of the gradients.  wide: those rows can be
+// written 16 bytes at a time.
+template <typename T, bool DELTA>
+__global__ void __launch_bounds__(256) attn_rows_kernel(AttnCall C, bool wide) {
+  pdl_trigger();                         // what follows works on other sequences
   const int t = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (t >= C.seqs.total) return;
   const Seqs& q = C.seqs;
@@ -312,18 +314,26 @@ __global__ void __launch_bounds__(256) attn_rows_kernel(AttnCall C) {
     alive = a < count && q.alive[a] == lo;
   }
   if (alive) {
-    for (int h = 0; h < C.heads_q; ++h) {
-      const T* o = (const T*)C.o.p + (int64_t)t * C.o.token + (int64_t)h * C.o.head;
-      const T* g = (const T*)C.d_o.p + (int64_t)t * C.d_o.token + (int64_t)h * C.d_o.head;
-      float s = 0.f;
-      for (int d = lane; d < C.dim; d += 32) s = fmaf(widen(o[d]), widen(g[d]), s);
-      s = warp_sum(s);
-      if (lane == 0) C.delta[(int64_t)h * q.total + t] = s;
-    }
+    if (DELTA)
+      for (int h = 0; h < C.heads_q; ++h) {
+        const T* o = (const T*)C.o.p + (int64_t)t * C.o.token + (int64_t)h * C.o.head;
+        const T* g = (const T*)C.d_o.p + (int64_t)t * C.d_o.token + (int64_t)h * C.d_o.head;
+        float s = 0.f;
+        for (int d = lane; d < C.dim; d += 32) s = fmaf(widen(o[d]), widen(g[d]), s);
+        s = warp_sum(s);
+        if (lane == 0) C.delta[(int64_t)h * q.total + t] = s;
+      }
   } else if (!C.skip_dropped) {
     auto zero = [&](const Strided& x, int heads) {
       T* base = (T*)const_cast<void*>(x.p) + (int64_t)t * x.token;
-      for (int i = lane; i < heads * C.dim; i += 32) put(base + (int64_t)(i / C.dim) * x.head + i % C.dim, 0.f);
+      constexpr int VN = 16 / sizeof(T);
+      if (wide) {
+        const int per = C.dim / VN;
+        for (int i = lane; i < heads * per; i += 32)
+          *reinterpret_cast<uint4*>(base + (int64_t)(i / per) * x.head + (i % per) * VN) = make_uint4(0, 0, 0, 0);
+      } else {
+        for (int i = lane; i < heads * C.dim; i += 32) put(base + (int64_t)(i / C.dim) * x.head + i % C.dim, 0.f);
+      }
     };
     zero(C.dq, C.heads_q);
     zero(C.dk, C.heads_kv);
@@ -382,17 +392,24 @@ cudaError_t launch_attn_fma_fwd(const Attn* a, const AttnCall& c, cudaStream_t s
     return c.dim <= 64 ? fwd<__nv_bfloat16, 64>(c, st) : fwd<__nv_bfloat16, 128>(c, st);
   return c.dim <= 64 ? fwd<float, 64>(c, st) : fwd<float, 128>(c, st);
 }
+template <bool DELTA>
+static cudaError_t rows(const Attn* a, const AttnCall& c, cudaStream_t st) {
+  const unsigned grid = (unsigned)((c.seqs.total + 7) / 8);
+  const int elem = a->desc.dtype == VCAS_DTYPE_BF16 ? 2 : 4, vn = 16 / elem;
+  auto wide = [&](const Strided& x) { return ((uintptr_t)x.p & 15) == 0 && x.token % vn == 0 && x.head % vn == 0; };
+  const bool w = wide(c.dq) && wide(c.dk) && wide(c.dv);
+  if (elem == 2) attn_rows_kernel<__nv_bfloat16, DELTA><<<grid, 256, 0, st>>>(c, w);
+  else attn_rows_kernel<float, DELTA><<<grid, 256, 0, st>>>(c, w);
+  return cudaGetLastError();
+}
 cudaError_t launch_attn_fma_bwd(const Attn* a, const AttnCall& c, cudaStream_t st) {
+  const cudaError_t e = rows<true>(a, c, st);
+  if (e != cudaSuccess) return e;
   if (a->desc.dtype == VCAS_DTYPE_BF16)
     return c.dim <= 64 ? bwd<__nv_bfloat16, 64>(c, st) : bwd<__nv_bfloat16, 128>(c, st);
   return c.dim <= 64 ? bwd<float, 64>(c, st) : bwd<float, 128>(c, st);
 }
-cudaError_t launch_attn_rows(const Attn* a, const AttnCall& c, cudaStream_t st) {
-  const unsigned grid = (unsigned)((c.seqs.total + 7) / 8);
-  if (a->desc.dtype == VCAS_DTYPE_BF16) attn_rows_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>(c);
-  else attn_rows_kernel<float><<<grid, 256, 0, st>>>(c);
-  return cudaGetLastError();
-}
+cudaError_t launch_attn_zero(const Attn* a, const AttnCall& c, cudaStream_t st) { return rows<false>(a, c, st); }
 
 }  // namespace vcas
 
@@ -430,6 +447,7 @@ extern "C" int vcas_attn_create(vcas_attn* out, const vcas_attn_desc* desc) {
   }
   a->delta = (float*)a->base;
   a->status = (int32_t*)((uint8_t*)a->base + delta);
+  a->next = a->status + 1;
   if (cudaMemset(a->base, 0, a->bytes) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
     cudaFree(a->base);
     delete a;
@@ -498,8 +516,7 @@ extern "C" int vcas_attn_bwd(vcas_attn aa, const vcas_attn_tensor* d_o, const vc
   DeviceScope on(a->device);
   if (!on.ok) return VCAS_ERR_CUDA;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  cudaError_t e = launch_attn_rows(a, c, st);
-  if (e == cudaSuccess) e = attn_umma_ok(a, c, true) ? launch_attn_umma_bwd(a, c, st) : launch_attn_fma_bwd(a, c, st);
+  const cudaError_t e = attn_umma_ok(a, c, true) ? launch_attn_umma_bwd(a, c, st) : launch_attn_fma_bwd(a, c, st);
   return e == cudaSuccess ? VCAS_OK : VCAS_ERR_CUDA;
 }
 

@@ -14,6 +14,7 @@ struct Attn {
   void* base;
   size_t bytes;
   float* delta;          // [heads_q][max_tokens] rowsum(dO O)
+  int32_t* next;         // tile counters of the tensor-core kernels, two for each
   int32_t* status;
   unsigned long long wait_limit_ns;
   int stall_once;
@@ -49,7 +50,7 @@ __device__ __forceinline__ float attn_exp2(float x) {
 
 // Sequence n: its first token and length; 0 tokens and a note in the status word where starts make no sense there.
 __device__ __forceinline__ int seq_length(const Seqs& q, int n, int& first) {
-  const int s = q.starts[n], e = q.starts[n + 1];
+  const int s = __ldcg(q.starts + n), e = __ldcg(q.starts + n + 1);   // past L1: a kernel may begin beside the one before it
   first = s;
   if (s < 0 || e < s || e > q.total) {
     atomicExch(q.status, (int32_t)VCAS_ERR_BAD_ARG);
@@ -59,7 +60,7 @@ __device__ __forceinline__ int seq_length(const Seqs& q, int n, int& first) {
 }
 __device__ __forceinline__ int seq_count(const Seqs& q) {
   if (q.alive == nullptr) return q.N;
-  const int c = *q.alive_cnt;
+  const int c = __ldcg(q.alive_cnt);
   if (c >= 0 && c <= q.N) return c;
   atomicExch(q.status, (int32_t)VCAS_ERR_BAD_ARG);
   return 0;
@@ -73,7 +74,7 @@ __device__ __forceinline__ bool find_tile(const Seqs& q, int tile, int rows, int
   for (int b = 0; b < count; b += 32) {
     int n = b + lane < count ? b + lane : -1, s = 0, l = 0;
     if (n >= 0 && q.alive != nullptr) {
-      n = q.alive[n];
+      n = __ldcg(q.alive + n);
       if (n < 0 || n >= q.N) {
         atomicExch(q.status, (int32_t)VCAS_ERR_BAD_ARG);
         n = -1;
@@ -105,8 +106,8 @@ inline long tile_bound(int total, int N, int rows) { return total / rows + (N < 
 
 cudaError_t launch_attn_fma_fwd(const Attn* a, const AttnCall& c, cudaStream_t st);
 cudaError_t launch_attn_fma_bwd(const Attn* a, const AttnCall& c, cudaStream_t st);
-// delta = rowsum(dO O) on the rows of the sequences that are worked on, zeros into dq, dk, dv on those of the others
-cudaError_t launch_attn_rows(const Attn* a, const AttnCall& c, cudaStream_t st);
+// Zeros into dq, dk, dv on the rows of the sequences that are not worked on.
+cudaError_t launch_attn_zero(const Attn* a, const AttnCall& c, cudaStream_t st);
 bool attn_umma_ok(const Attn* a, const AttnCall& c, bool backward);
 cudaError_t launch_attn_umma_fwd(const Attn* a, const AttnCall& c, cudaStream_t st);
 cudaError_t launch_attn_umma_bwd(const Attn* a, const AttnCall& c, cudaStream_t st);

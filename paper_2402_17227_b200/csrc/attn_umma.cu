@@ -1,10 +1,10 @@
 // Attention over packed sequences on the tensor cores (bf16, tcgen05): one forward and two backward kernels.
 //
-// A CTA owns a tile of 128 rows of one head and walks over the tiles of the other side.  One warp loads tiles with TMA, one lane
-// issues the products, four (forward) or eight (backward) warps turn scores into probabilities, a row of TMEM being a lane's
-// own.  Scores stay in TMEM; P and dS go back there as bf16, over the scores they came from, and are the A operand of the
-// product that follows.  tcgen05.mma of one thread run in order, so a tile of scores may be overwritten by the next
-// product as soon as the product that reads it is issued.
+// A CTA stays for as long as there are tiles of 128 rows of one head to be had, and walks each against the tiles of the other
+// side.  One warp takes tiles from a counter and loads with TMA, ahead of the others and across tiles; one lane issues the products;
+// four or eight warps turn scores into probabilities, a row of TMEM being a lane's own.  Scores stay in TMEM; P and dS go back
+// there as bf16, over the scores they came from, and are the A operand of the product that follows.  tcgen05.mma of one thread run in
+// order, so a tile of scores may be overwritten by the next product as soon as the product that reads it is issued.
 //   forward    S = Q K^T,  P = exp(S - m),  O += P V; O is rescaled only where the maximum rose by more than 2^8
 //   dQ         rows are queries: S, dP = dO V^T, dS = P (dP - delta), dQ += dS K
 //   dK, dV     rows are keys:    S^T = K Q^T, dV += P^T dO, dP^T = V dO^T, dK += dS^T Q, over all query heads of the group
@@ -16,7 +16,8 @@
 namespace vcas {
 namespace {
 
-constexpr int CHUNK = 128 * 64 * 2;      // 128 rows of 64 bf16: one 128-byte swizzled block
+// A tile of ROWS rows is one block of 128-byte swizzled rows (64 bf16) for each 64 of its columns.
+template <int ROWS> constexpr int CHUNK = ROWS * 64 * 2;
 
 // ------------------------------------------------------------------------------- TMEM and operands
 // 32 lanes x 64 columns
@@ -53,79 +54,127 @@ __device__ __forceinline__ void umma_bf16_ts(uint32_t tmem_d, uint32_t tmem_a, u
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
       ::"r"(tmem_d), "r"(tmem_a), "l"(desc_b), "r"(idesc), "r"(accumulate) : "memory");
 }
-// A tile of 128 rows is CHUNK bytes for each 64 columns.  Its rows as the summed-over side of a product: 64-wide chunks CHUNK apart.
+// A tile's rows as the summed-over side of a product: its 64-wide blocks lie CHUNK apart.
+template <int ROWS>
 __device__ __forceinline__ uint64_t desc_rows(uint32_t saddr) {
-  return (uint64_t)((saddr & 0x3ffffu) >> 4) | ((uint64_t)(CHUNK >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+  return (uint64_t)((saddr & 0x3ffffu) >> 4) | ((uint64_t)(CHUNK<ROWS> >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
-// D [128 x 128] = A B^T, both tiles of 128 rows, summed over their 64 * DC columns
-template <int DC>
+// D [128 x TN] = A B^T, tiles of 128 and TN rows, summed over their 64 * DC columns
+template <int DC, int TN>
 __device__ __forceinline__ void product_tiles(uint32_t d, uint32_t a, uint32_t b) {
-  constexpr uint32_t idesc = make_idesc(128, false, false);
+  constexpr uint32_t idesc = make_idesc(TN, false, false);
 #pragma unroll
   for (int c = 0; c < DC; ++c) {
-    const uint64_t da = desc_kmajor(a + c * CHUNK), db = desc_kmajor(b + c * CHUNK);
+    const uint64_t da = desc_kmajor(a + c * CHUNK<128>), db = desc_kmajor(b + c * CHUNK<TN>);
 #pragma unroll
     for (int k = 0; k < 4; ++k) umma_bf16(d, da + (uint64_t)(k * 2), db + (uint64_t)(k * 2), idesc, (c | k) != 0 ? 1u : 0u);
   }
 }
-// D [128 x 64 DC] (+)= A B, A [128 x 128] bf16 in TMEM (its upper 64 columns `gap` TMEM columns behind the lower), B a tile
-template <int DC>
+// D [128 x 64 DC] (+)= A B, A [128 x TN] bf16 in TMEM (each 64 of its columns `gap` TMEM columns behind the 64 before), B a tile of
+// TN rows
+template <int DC, int TN, int K0, int K1>           // columns 16 K0 .. 16 K1 of A
 __device__ __forceinline__ void product_rows(uint32_t d, uint32_t a, int gap, uint32_t b, bool add) {
   constexpr uint32_t idesc = make_idesc(64 * DC, false, true);
-  const uint64_t db = desc_rows(b);
+  const uint64_t db = desc_rows<TN>(b);
 #pragma unroll
-  for (int k = 0; k < 8; ++k)
+  for (int k = K0; k < K1; ++k)
     umma_bf16_ts(d, a + (uint32_t)((k & 3) * 8 + (k >> 2) * gap), db + (uint64_t)(k * (16 * 128 >> 4)), idesc, add || k != 0 ? 1u : 0u);
 }
-// rows have .. 127 of a tile become 0, by one warp; the products after it see them
-template <int DC>
+// the rows from `have` on of a tile become 0, by one warp; the products after it see them
+template <int DC, int ROWS>
 __device__ __forceinline__ void zero_rows(uint8_t* tile, int have, int lane) {
-  for (int i = have * 8 + lane; i < 128 * 8; i += 32)
+  for (int i = have * 8 + lane; i < ROWS * 8; i += 32)
 #pragma unroll
-    for (int c = 0; c < DC; ++c) *reinterpret_cast<uint4*>(tile + c * CHUNK + i * 16) = make_uint4(0, 0, 0, 0);
+    for (int c = 0; c < DC; ++c) *reinterpret_cast<uint4*>(tile + c * CHUNK<ROWS> + i * 16) = make_uint4(0, 0, 0, 0);
 }
-template <int DC>
+template <int DC, int ROWS>
 __device__ __forceinline__ void load_tile(uint8_t* dst, const CUtensorMap* map, int head, int token, uint64_t* bar) {
 #pragma unroll
-  for (int c = 0; c < DC; ++c) tma_load_3d(dst + c * CHUNK, map, 64 * c, head, token, bar);
+  for (int c = 0; c < DC; ++c) tma_load_3d(dst + c * CHUNK<ROWS>, map, 64 * c, head, token, bar);
+}
+// sum over a row of two tiles of 128 rows of their products
+template <int DC>
+__device__ __forceinline__ float row_dot(const uint8_t* a, const uint8_t* b, int row) {
+  float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+  for (int c = 0; c < DC; ++c)
+#pragma unroll
+    for (int v = 0; v < 8; ++v) {
+      const int at = c * CHUNK<128> + row * 128 + ((v ^ (row & 7)) << 4);          // the 128-byte swizzle
+      const uint4 x = *reinterpret_cast<const uint4*>(a + at), y = *reinterpret_cast<const uint4*>(b + at);
+      const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s0 = fmaf(__uint_as_float(xs[e] << 16), __uint_as_float(ys[e] << 16), s0);
+        s1 = fmaf(__uint_as_float(xs[e] & 0xffff0000u), __uint_as_float(ys[e] & 0xffff0000u), s1);
+      }
+    }
+  return s0 + s1;
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&t);
 }
-// this lane's row of a [128 x 64 DC] accumulator, times f, to a row of a tensor
+// A warp's 32 rows of a [128 x 64 DC] accumulator, times f (each lane its row's), to rows of a tensor; `rows` of them exist.  Four lanes
+// exchange 16-byte pieces of their rows, so that a store instruction writes 64 bytes in a row (a lane writing its own row, 16 bytes of 32
+// rows at a time, took 1.4 us a tile, half as long as a tile of scores).
 template <int DC>
-__device__ __forceinline__ void store_row(uint32_t taddr, __nv_bfloat16* row, int dim, bool in, float f) {
+__device__ __forceinline__ void store_rows(uint32_t taddr, const Strided& x, int64_t first, int head, int dim, int rows, float f) {
+  const int lane = threadIdx.x & 31, unit = lane & 3;
+  __nv_bfloat16* base = (__nv_bfloat16*)const_cast<void*>(x.p) + (first + (lane & ~3)) * x.token + (int64_t)head * x.head + unit * 8;
 #pragma unroll
   for (int c = 0; c < 2 * DC; ++c) {
-    uint32_t v[32];
+    uint32_t v[32], u[4][4];
     tmem_ld32(taddr + c * 32, v);
 #pragma unroll
-    for (int e = 0; e < 32; e += 8) {
-      const int d = c * 32 + e;
-      if (in && d < dim) {
-        uint32_t o[4];
+    for (int k = 0; k < 4; ++k)
 #pragma unroll
-        for (int h = 0; h < 4; ++h) o[h] = pack_bf16(__uint_as_float(v[e + 2 * h]) * f, __uint_as_float(v[e + 2 * h + 1]) * f);
-        *reinterpret_cast<uint4*>(row + d) = make_uint4(o[0], o[1], o[2], o[3]);
+      for (int e = 0; e < 4; ++e) u[k][e] = pack_bf16(__uint_as_float(v[8 * k + 2 * e]) * f, __uint_as_float(v[8 * k + 2 * e + 1]) * f);
+    // the 4 x 4 pieces of four lanes, turned over
+    auto swap = [&](uint32_t (&lo)[4], uint32_t (&hi)[4], int bit) {
+      const bool up = (lane & bit) != 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? lo[e] : hi[e], bit);
+        if (up) lo[e] = got; else hi[e] = got;
       }
+    };
+    swap(u[0], u[1], 1);
+    swap(u[2], u[3], 1);
+    swap(u[0], u[2], 2);
+    swap(u[1], u[3], 2);
+    if (c * 32 + unit * 8 < dim) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if ((lane & ~3) + k < rows)
+          *reinterpret_cast<uint4*>(base + (int64_t)k * x.token + c * 32) = make_uint4(u[k][0], u[k][1], u[k][2], u[k][3]);
     }
   }
 }
 
 // ----------------------------------------------------------------------------------------- the CTA
-constexpr int MAX_STAGES = 4;
+constexpr int MAX_STAGES = 6;
+struct Item { int first, len, t0, head, any; };      // a tile of 128 rows: its sequence, its first row in there, its head
 struct Shared {
-  uint64_t full[MAX_STAGES], empty[MAX_STAGES], own, scores[2], dscores, ready[2], done, drain;
+  uint64_t full[MAX_STAGES], empty[MAX_STAGES];      // ring of the other side's tiles
+  uint64_t item_full[2], item_empty[2];
+  uint64_t own_full, own_empty;                      // the item's own tiles
+  uint64_t scores[2], dscores;                       // products of which the scores' warps wait
+  uint64_t ready[2];                                 // P, dS written
+  uint64_t done, acc_empty;                          // accumulators complete, and read
+  uint64_t o_read, drain;
+  uint64_t rows_full[2][2];                          // dK, dV: the queries' values, by column half and buffer
   uint32_t tmem;
-  int abort_flag;                        // mbar_wait finds the limit 20 bytes behind it
-  int first, len, t0, any;
+  int abort_flag;                                    // mbar_wait finds the limit 20 bytes behind it
+  int pad[4];
   unsigned long long limit;
+  Item item[2];
 };
 static_assert(offsetof(Shared, limit) == offsetof(Shared, abort_flag) + 20, "see mbar_wait");
 
 struct UmmaCall {
   AttnCall c;
+  int32_t* next;                                     // two counters: tiles taken, CTAs that are through
   unsigned long long wait_limit_ns;
   int stall_once;
 };
@@ -134,57 +183,140 @@ struct UmmaCall {
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* ab, int32_t* status) {
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, ab, status));
 }
+__device__ __forceinline__ void warp_arrive(uint64_t* bar) {
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) mbar_arrive(bar);
+}
 
-// Finds the CTA's tile, sets the barriers up and takes TMEM; false where there is no tile.
-__device__ __forceinline__ bool begin(Shared& s, const UmmaCall& P, int heads, bool last_first, int stages, uint32_t readers, uint32_t columns) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (warp == 0) {
-    int first = 0, len = 0, place = 0;
-    const bool any = find_tile(P.c.seqs, (int)(blockIdx.x / (unsigned)heads), 128, lane, first, len, place);
-    if (lane == 0) {
-      s.first = first; s.len = len; s.any = any;
-      s.t0 = (last_first ? (len + 127) / 128 - 1 - place : place) * 128;
-    }
-  } else if (warp == 1 && lane == 0) {
+// Shared memory is all dynamic, its tiles first: they have to begin on a 1024-byte boundary, where the CTA's part begins.
+__device__ __forceinline__ bool in_place(const uint8_t* smem, int32_t* status) {
+  if ((smem_u32(smem) & 1023u) == 0) return true;
+  if (threadIdx.x == 0) atomicExch(status, (int32_t)VCAS_ERR_INTERNAL);
+  return false;
+}
+// Sets the barriers up and takes TMEM.  warps: those that work on scores.
+__device__ __forceinline__ void begin(Shared& s, const UmmaCall& P, int stages, uint32_t warps, uint32_t own_readers, uint32_t columns) {
+  if (threadIdx.x == 0) {
     for (int i = 0; i < stages; ++i) { mbar_init(&s.full[i], 1); mbar_init(&s.empty[i], 1); }
-    mbar_init(&s.own, 1);
-    mbar_init(&s.scores[0], 1);
-    mbar_init(&s.scores[1], 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&s.item_full[i], 1);
+      mbar_init(&s.item_empty[i], warps + 1);
+      mbar_init(&s.scores[i], 1);
+      mbar_init(&s.ready[i], warps);
+    }
+    mbar_init(&s.own_full, 1);
+    mbar_init(&s.own_empty, 1 + own_readers);
     mbar_init(&s.dscores, 1);
-    mbar_init(&s.ready[0], readers);
-    mbar_init(&s.ready[1], readers);
     mbar_init(&s.done, 1);
+    mbar_init(&s.acc_empty, warps);
+    mbar_init(&s.o_read, warps);
+    for (int i = 0; i < 4; ++i) mbar_init(&s.rows_full[i >> 1][i & 1], 4);
     mbar_init(&s.drain, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     s.abort_flag = 0;
     s.limit = P.wait_limit_ns;
   }
-  __syncthreads();
-  if (!s.any) return false;
-  if (warp == 2) tmem_alloc(&s.tmem, columns);
+  if ((threadIdx.x >> 5) == 2) tmem_alloc(&s.tmem, columns);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  return true;
 }
-__device__ __forceinline__ void end(Shared& s, uint32_t columns) {
+__device__ __forceinline__ void end(Shared& s, const UmmaCall& P, uint32_t columns) {
   tc_fence_before();
   __syncthreads();
   if ((threadIdx.x >> 5) == 2) {
     tc_fence_after();
     tmem_dealloc(s.tmem, columns);
   }
+  // the last CTA leaves the counters as it found them
+  if (threadIdx.x == 0 && atomicAdd(P.next + 1, 1) == (int)gridDim.x - 1) {
+    P.next[0] = 0;
+    P.next[1] = 0;
+  }
 }
 // A ring position
 struct Ring {
   int stage = 0;
   uint32_t phase = 0;
+  uint32_t filled = 0;
   __device__ __forceinline__ void next(int stages) {
     if (++stage == stages) { stage = 0; phase ^= 1u; }
   }
 };
+// The loading warp's part: takes the next tile off the counter and tells the others.  The counter goes through the heads first, then
+// through the tiles of a sequence (last_first: from its end), so that CTAs at work at the same time share the other side's tiles.
+__device__ __forceinline__ bool take_item(Shared& s, const UmmaCall& P, int n, int heads, bool last_first, Item& it) {
+  const int lane = threadIdx.x & 31;
+  volatile int* ab = &s.abort_flag;
+  if (!warp_wait(&s.item_empty[n & 1], ((n >> 1) & 1) ^ 1, ab, P.c.seqs.status)) return false;
+  int at = 0;
+  if (lane == 0) at = atomicAdd(P.next, 1);
+  at = __shfl_sync(0xffffffffu, at, 0);
+  int place = 0;
+  it.first = it.len = 0;
+  it.head = at % heads;
+  it.any = find_tile(P.c.seqs, at / heads, 128, lane, it.first, it.len, place);
+  it.t0 = (last_first ? (it.len + 127) / 128 - 1 - place : place) * 128;
+  if (lane == 0) {
+    s.item[n & 1] = it;
+    mbar_arrive(&s.item_full[n & 1]);
+  }
+  return it.any;
+}
+// The others' part.  False: no more, or given up.
+__device__ __forceinline__ bool get_item(Shared& s, int n, int32_t* status, Item& it) {
+  if (!warp_wait(&s.item_full[n & 1], (n >> 1) & 1, &s.abort_flag, status)) return false;
+  it = s.item[n & 1];
+  warp_arrive(&s.item_empty[n & 1]);
+  return it.any;
+}
+// Loads a tile of the ring; `skip`: the test hook that leaves the copy out.
+template <int DC, int ROWS>
+__device__ __forceinline__ bool fill(Shared& s, Ring& r, int stages, uint8_t* ring, const CUtensorMap* map, int head, int token, bool skip,
+                                     int32_t* status) {
+  constexpr int BYTES = DC * CHUNK<ROWS>;
+  if (!warp_wait(&s.empty[r.stage], r.phase ^ 1u, &s.abort_flag, status)) return false;
+  if (!skip) {
+    if (elect_one()) {
+      mbar_expect_tx(&s.full[r.stage], BYTES);
+      load_tile<DC, ROWS>(ring + r.stage * BYTES, map, head, token, &s.full[r.stage]);
+    }
+    ++r.filled;
+  }
+  r.next(stages);
+  return true;
+}
+// After a wait that ran out: nothing may arrive in shared memory that is no longer this CTA's.
+__device__ __forceinline__ void drain(Shared& s, const Ring& r, int stages, uint32_t own_filled, int32_t* status) {
+  if (!*(volatile int*)&s.abort_flag) return;
+  if (own_filled != 0) mbar_wait(&s.own_full, (own_filled - 1) & 1, &s.abort_flag, status);
+  drain_loads(s.full, stages, r.stage, r.phase, r.filled, &s.abort_flag, status);
+}
 
 // ------------------------------------------------------------------------------------------ forward
+// 2^x by the FMA pipe: x = n + f, |f| <= 1/2, n goes to the exponent, 2^f by the polynomial of degree 5 with the least largest relative
+// error there (7.5e-8, by Remez exchange).  x is at most about 8; below -127 the result is under 2^-126.
+__device__ __forceinline__ void exp2_poly(float x0, float x1, float& y0, float& y1) {
+  float c0, c1;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(c0) : "f"(x0), "f"(-127.0f));
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(c1) : "f"(x1), "f"(-127.0f));
+  const uint64_t x = pack2(c0, c1);
+  const uint64_t big = pack2(12582912.0f, 12582912.0f), nbig = pack2(-12582912.0f, -12582912.0f), neg = pack2(-1.0f, -1.0f);
+  const uint64_t t = add2(x, big);                   // n in the low bits of the mantissa
+  const uint64_t f = fma2(add2(t, nbig), neg, x);
+  uint64_t p = fma2(f, pack2(1.3276476e-3f, 1.3276476e-3f), pack2(9.675541e-3f, 9.675541e-3f));
+  p = fma2(p, f, pack2(5.550713e-2f, 5.550713e-2f));
+  p = fma2(p, f, pack2(0.2402212f, 0.2402212f));
+  p = fma2(p, f, pack2(0.69314694f, 0.69314694f));
+  p = fma2(p, f, pack2(1.0000001f, 1.0000001f));
+  float t0, t1, p0, p1;
+  unpack2(t, t0, t1);
+  unpack2(p, p0, p1);
+  y0 = __uint_as_float(__float_as_uint(p0) + (__float_as_uint(t0) << 23));
+  y1 = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(t1) << 23));
+}
+constexpr int POLY_OF_8 = 2;      // of eight pairs of exponentials, how many go to the FMA pipe
+
 // Two CTAs an SM, each with 128 query rows: while one turns scores into probabilities the other's products run.  K and V tiles take
 // turns in the ring; a score tile takes 128 columns of TMEM and O another 64 DC.
 template <int DC> constexpr int FWD_STAGES = DC == 1 ? 4 : 2;
@@ -194,528 +326,649 @@ template <int DC>
 __global__ void __launch_bounds__(FWD_THREADS, 2)
 attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                 const __grid_constant__ UmmaCall P) {
-  constexpr int STAGES = FWD_STAGES<DC>, TILE_BYTES = DC * CHUNK;
-  extern __shared__ uint8_t raw[];
-  __shared__ Shared s;
-  uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
-  uint8_t *sq = smem, *ring = smem + TILE_BYTES;
+  constexpr int STAGES = FWD_STAGES<DC>, TILE = DC * CHUNK<128>;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  uint8_t *sq = smem, *ring = smem + TILE;
+  Shared& s = *reinterpret_cast<Shared*>(ring + STAGES * TILE);
   const AttnCall& C = P.c;
-  if (!begin(s, P, C.heads_q, C.causal, STAGES, 128, 256)) return;
+  if (!in_place(smem, C.seqs.status)) return;
+  begin(s, P, STAGES, 4, 0, 256);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int head = (int)(blockIdx.x % (unsigned)C.heads_q), first = s.first, len = s.len, t0 = s.t0;
-  const int end_col = C.causal ? min(len, t0 + 128) : len, tiles = (end_col + 127) / 128;
   const uint32_t ts = s.tmem, to = s.tmem + 128;
   volatile int* ab = &s.abort_flag;
   int32_t* status = C.seqs.status;
+  auto tiles_of = [&](const Item& it) { return ((C.causal ? min(it.len, it.t0 + 128) : it.len) + 127) / 128; };
 
   if (warp == 5) {
-    if (elect_one()) {
-      mbar_expect_tx(&s.own, TILE_BYTES);
-      load_tile<DC>(sq, &mq, head, first + t0, &s.own);
-      Ring r;
-      uint32_t filled = 0;
-      const int kv = head / C.group;
-      bool ok = true;
-      for (int i = 0; i < 2 * tiles && ok; ++i) {
-        ok = mbar_wait(&s.empty[r.stage], r.phase ^ 1u, ab, status);
-        if (!ok) break;
-        if (P.stall_once && blockIdx.x == 0 && i == 0) { r.next(STAGES); continue; }
-        mbar_expect_tx(&s.full[r.stage], TILE_BYTES);
-        load_tile<DC>(ring + r.stage * TILE_BYTES, (i & 1) ? &mv : &mk, kv, first + (i >> 1) * 128, &s.full[r.stage]);
-        r.next(STAGES);
-        ++filled;
+    Ring r;
+    Item it;
+    uint32_t own = 0;
+    for (int n = 0; take_item(s, P, n, C.heads_q, C.causal, it); ++n) {
+      bool ok = warp_wait(&s.own_empty, (n & 1) ^ 1, ab, status);
+      if (!ok) break;
+      if (elect_one()) {
+        mbar_expect_tx(&s.own_full, TILE);
+        load_tile<DC, 128>(sq, &mq, it.head, it.first + it.t0, &s.own_full);
       }
-      if (*ab) {
-        mbar_wait(&s.own, 0, ab, status);
-        drain_loads(s.full, STAGES, r.stage, r.phase, filled, ab, status);
-      }
+      ++own;
+      const int tiles = tiles_of(it), kv = it.head / C.group;
+      const bool stall = P.stall_once && blockIdx.x == 0 && n == 0;
+      for (int i = 0; i < 2 * tiles && ok; ++i)
+        ok = fill<DC, 128>(s, r, STAGES, ring, (i & 1) ? &mv : &mk, kv, it.first + (i >> 1) * 128, stall && i == 0, status);
+      if (!ok) break;
     }
+    if (lane == 0) drain(s, r, STAGES, own, status);
   } else if (warp == 4) {
     const bool leader = elect_one();
-    bool ok = warp_wait(&s.own, 0, ab, status);
     Ring r;
-    for (int j = 0; j < tiles && ok; ++j) {
-      ok = warp_wait(&s.full[r.stage], r.phase, ab, status);
-      if (!ok) break;
-      tc_fence_after();
-      if (leader) {
-        product_tiles<DC>(ts, smem_u32(sq), smem_u32(ring + r.stage * TILE_BYTES));
-        umma_commit(&s.empty[r.stage]);
-        umma_commit(&s.scores[0]);
+    Item it;
+    uint32_t made = 0;                   // P tiles so far
+    bool ok = true;
+    for (int n = 0; ok && get_item(s, n, status, it); ++n) {
+      const int tiles = tiles_of(it);
+      ok = warp_wait(&s.own_full, n & 1, ab, status);
+      for (int j = 0; j < tiles && ok; ++j, ++made) {
+        ok = warp_wait(&s.full[r.stage], r.phase, ab, status);
+        if (!ok) break;
+        tc_fence_after();
+        if (leader) {
+          product_tiles<DC, 128>(ts, smem_u32(sq), smem_u32(ring + r.stage * TILE));
+          umma_commit(&s.empty[r.stage]);
+          umma_commit(&s.scores[0]);
+          if (j == tiles - 1) umma_commit(&s.own_empty);
+        }
+        r.next(STAGES);
+        ok = warp_wait(&s.full[r.stage], r.phase, ab, status);
+        if (!ok) break;
+        uint8_t* v = ring + r.stage * TILE;
+        const int have = it.len - j * 128;
+        if (have < 128) {
+          zero_rows<DC, 128>(v, have, lane);
+          fence_async_smem();
+          __syncwarp();
+        }
+        if (j == 0) ok = warp_wait(&s.acc_empty, (n & 1) ^ 1, ab, status);
+        // the lower half of P's columns, then the upper, as they come
+        ok = ok && warp_wait(&s.ready[0], made & 1, ab, status);
+        if (!ok) break;
+        tc_fence_after();
+        if (leader) product_rows<DC, 128, 0, 4>(to, ts, 32, smem_u32(v), j != 0);
+        ok = warp_wait(&s.ready[1], made & 1, ab, status);
+        if (!ok) break;
+        tc_fence_after();
+        if (leader) {
+          product_rows<DC, 128, 4, 8>(to, ts, 32, smem_u32(v), true);
+          umma_commit(&s.empty[r.stage]);
+          if (j == tiles - 1) umma_commit(&s.done);
+        }
+        r.next(STAGES);
       }
-      r.next(STAGES);
-      ok = warp_wait(&s.full[r.stage], r.phase, ab, status);
-      if (!ok) break;
-      if (len - j * 128 < 128) {
-        zero_rows<DC>(ring + r.stage * TILE_BYTES, len - j * 128, lane);
-        fence_async_smem();
-        __syncwarp();
-      }
-      ok = warp_wait(&s.ready[0], j & 1, ab, status);
-      if (!ok) break;
-      tc_fence_after();
-      if (leader) {
-        product_rows<DC>(to, ts, 32, smem_u32(ring + r.stage * TILE_BYTES), j != 0);
-        umma_commit(&s.empty[r.stage]);
-      }
-      r.next(STAGES);
     }
-    if (leader) {
-      if (ok) umma_commit(&s.done);
-      else drain_products(&s.drain, ab, status);
-    }
+    if (leader && *ab) drain_products(&s.drain, ab, status);
   } else {
-    const int row = t0 + threadIdx.x;                // in the sequence
     const uint32_t lanes = (uint32_t)(warp * 32) << 16;
     const float c = C.scale * ATTN_LOG2E, none = __int_as_float(0xff800000);
-    float m = none, l = 0.f;
+    Item it;
+    uint32_t made = 0;
     bool ok = true;
-    for (int j = 0; j < tiles; ++j) {
-      ok = warp_wait(&s.scores[0], j & 1, ab, status);
-      if (!ok) break;
-      tc_fence_after();
-      uint32_t a[64], b[64];
-      tmem_ld64(ts + lanes, a);
-      tmem_ld64(ts + lanes + 64, b);
-      // columns this row sees in the tile
-      const int see = min(128, (C.causal ? min(len, row + 1) : len) - j * 128);
-      if (__any_sync(0xffffffffu, see < 128)) {
+    for (int n = 0; ok && get_item(s, n, status, it); ++n) {
+      const int row = it.t0 + threadIdx.x, tiles = tiles_of(it);         // row: in the sequence
+      float m = none, l = 0.f;
+      for (int j = 0; j < tiles; ++j, ++made) {
+        ok = warp_wait(&s.scores[0], made & 1, ab, status);
+        if (!ok) break;
+        tc_fence_after();
+        uint32_t a[64], b[64];
+        tmem_ld64(ts + lanes, a);
+        tmem_ld64(ts + lanes + 64, b);
+        // columns this row sees in the tile
+        const int see = min(128, (C.causal ? min(it.len, row + 1) : it.len) - j * 128);
+        const bool cut = __any_sync(0xffffffffu, see < 128);
+        if (cut) {
 #pragma unroll
-        for (int i = 0; i < 64; ++i) {
-          a[i] = i < see ? a[i] : 0xff800000u;
-          b[i] = i + 64 < see ? b[i] : 0xff800000u;
-        }
-      }
-      float t[4] = {none, none, none, none};
-#pragma unroll
-      for (int i = 0; i < 64; ++i) t[i & 3] = fmaxf(t[i & 3], fmaxf(__uint_as_float(a[i]), __uint_as_float(b[i])));
-      const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
-      if (j == 0) {
-        m = top;
-      } else {
-        // the sums are relative to m; it follows the maximum once that has risen far enough for P to lose range
-        const bool rise = (top - m) * c > 8.0f;
-        if (__any_sync(0xffffffffu, rise)) {
-          const float f = rise ? attn_exp2((m - top) * c) : 1.0f;
-          m = rise ? top : m;
-          l *= f;
-#pragma unroll
-          for (int q = 0; q < 2 * DC; ++q) {
-            uint32_t o[32];
-            tmem_ld32(to + lanes + q * 32, o);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-            tmem_st32(to + lanes + q * 32, o);
+          for (int i = 0; i < 64; ++i) {
+            a[i] = i < see ? a[i] : 0xff800000u;
+            b[i] = i + 64 < see ? b[i] : 0xff800000u;
           }
         }
-      }
-      const float ref = m == none ? 0.f : m;
-      const uint64_t c2 = pack2(c, c), n2 = pack2(-ref * c, -ref * c);
-      uint64_t l2[2] = {0, 0};
-      auto half = [&](const uint32_t (&x)[64], uint32_t at) {
-        uint32_t o[32];
+        float t[4] = {none, none, none, none};
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          float e0, e1;
-          unpack2(fma2(pack2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), c2, n2), e0, e1);
-          e0 = attn_exp2(e0);
-          e1 = attn_exp2(e1);
-          l2[i & 1] = add2(l2[i & 1], pack2(e0, e1));
-          o[i] = pack_bf16(e0, e1);
+        for (int i = 0; i < 64; ++i) t[i & 3] = fmaxf(t[i & 3], fmaxf(__uint_as_float(a[i]), __uint_as_float(b[i])));
+        const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+        if (j == 0) {
+          m = top;
+        } else {
+          // the sums are relative to m; it follows the maximum once that has risen far enough for P to lose range
+          const bool rise = (top - m) * c > 8.0f;
+          if (__any_sync(0xffffffffu, rise)) {
+            const float f = rise ? attn_exp2((m - top) * c) : 1.0f;
+            m = rise ? top : m;
+            l *= f;
+#pragma unroll
+            for (int q = 0; q < 2 * DC; ++q) {
+              uint32_t o[32];
+              tmem_ld32(to + lanes + q * 32, o);
+#pragma unroll
+              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+              tmem_st32(to + lanes + q * 32, o);
+            }
+          }
         }
-        tmem_st32(at, o);
-      };
-      half(a, ts + lanes);
-      half(b, ts + lanes + 32);
-      float x0, x1;
-      unpack2(add2(l2[0], l2[1]), x0, x1);
-      l += x0 + x1;
-      tmem_wait_st();
-      tc_fence_before();
-      mbar_arrive(&s.ready[0]);
-    }
-    ok = ok && warp_wait(&s.done, 0, ab, status);
-    if (ok) {
+        const float ref = m == none ? 0.f : m;
+        const uint64_t c2 = pack2(c, c), n2 = pack2(-ref * c, -ref * c);
+        uint64_t l2[2] = {0, 0};
+        auto half = [&](const uint32_t (&x)[64], uint32_t at, uint64_t* bar, bool poly) {
+          uint32_t o[32];
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            float e0, e1;
+            unpack2(fma2(pack2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), c2, n2), e0, e1);
+            if (poly && (i * POLY_OF_8) % 8 < POLY_OF_8) {
+              exp2_poly(e0, e1, e0, e1);
+            } else {
+              e0 = attn_exp2(e0);
+              e1 = attn_exp2(e1);
+            }
+            l2[i & 1] = add2(l2[i & 1], pack2(e0, e1));
+            o[i] = pack_bf16(e0, e1);
+          }
+          tmem_st32(at, o);
+          tmem_wait_st();
+          tc_fence_before();
+          warp_arrive(bar);
+        };
+        if (cut) {                       // masked places have to become 0 exactly
+          half(a, ts + lanes, &s.ready[0], false);
+          half(b, ts + lanes + 32, &s.ready[1], false);
+        } else {
+          half(a, ts + lanes, &s.ready[0], true);
+          half(b, ts + lanes + 32, &s.ready[1], true);
+        }
+        float x0, x1;
+        unpack2(add2(l2[0], l2[1]), x0, x1);
+        l += x0 + x1;
+      }
+      ok = ok && warp_wait(&s.done, n & 1, ab, status);
+      if (!ok) break;
       tc_fence_after();
-      __nv_bfloat16* o = (__nv_bfloat16*)const_cast<void*>(C.o.p) + (int64_t)(first + row) * C.o.token + (int64_t)head * C.o.head;
-      store_row<DC>(to + lanes, o, C.dim, row < len, 1.0f / l);
-      if (row < len) C.lse[(int64_t)head * C.seqs.total + first + row] = (m * c) * ATTN_LN2 + logf(l);
+      store_rows<DC>(to + lanes, C.o, (int64_t)it.first + it.t0 + warp * 32, it.head, C.dim, it.len - it.t0 - warp * 32, 1.0f / l);
+      tc_fence_before();
+      warp_arrive(&s.acc_empty);
+      if (row < it.len) C.lse[(int64_t)it.head * C.seqs.total + it.first + row] = (m * c) * ATTN_LN2 + logf(l);
     }
   }
-  end(s, 256);
+  end(s, P, 256);
 }
 
 // ------------------------------------------------------------------------------------------ backward
-constexpr int BWD_THREADS = 320;         // eight warps for the scores: 32 rows and 64 columns each
+// The other side comes in tiles of TN rows.  Heads of up to 64: 64, which leaves room for two CTAs an SM (TMEM holds 256 columns of
+// each), so that one computes while the other starts, waits or stores.  Wider ones: 128, one CTA.  A warp has 32 rows and 64 columns of
+// scores.  The ring's tiles are used two at a time and given back one by one: with five, the tiles of the next step are on their way
+// one step ahead.
+template <int DC> constexpr int TN_OF = DC == 1 ? 64 : 128;
+template <int DC> constexpr int BWD_WARPS = 4 * TN_OF<DC> / 64;
+template <int DC> constexpr int BWD_THREADS = 32 * (BWD_WARPS<DC> + 2);
+template <int DC> constexpr int BWD_CTAS = DC == 1 ? 2 : 1;
+template <int DC> constexpr int BWD_STAGES = DC == 1 ? 6 : 5;
 
-// Rows are queries.  TMEM: two score tiles in turn (dS replaces its own), dP, dQ.
+// Rows are queries.  TMEM: two score tiles in turn (dS replaces its own), dP, dQ.  O comes once, for delta = rowsum(dO O): in the ring
+// where its tiles are as large (DC = 2), else beside Q and dO.
 template <int DC>
-__global__ void __launch_bounds__(BWD_THREADS, 1)
-attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mdo, const __grid_constant__ CUtensorMap mk,
-               const __grid_constant__ CUtensorMap mv, const __grid_constant__ UmmaCall P) {
-  constexpr int STAGES = 2, TILE_BYTES = DC * CHUNK;
-  extern __shared__ uint8_t raw[];
-  __shared__ Shared s;
-  uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
-  uint8_t *sq = smem, *sdo = smem + TILE_BYTES, *ring = smem + 2 * TILE_BYTES;      // a stage: K, V
+__global__ void __launch_bounds__(BWD_THREADS<DC>, BWD_CTAS<DC>)
+attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mdo, const __grid_constant__ CUtensorMap mo,
+               const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const __grid_constant__ UmmaCall P) {
+  constexpr int STAGES = BWD_STAGES<DC>, TN = TN_OF<DC>, WARPS = BWD_WARPS<DC>, OWN = DC * CHUNK<128>, TILE = DC * CHUNK<TN>;
+  constexpr bool O_IN_RING = DC == 2;
+  static_assert(!O_IN_RING || TN == 128, "as large as a tile of the ring");
+  extern __shared__ __align__(1024) uint8_t smem[];
+  uint8_t *sq = smem, *sdo = sq + OWN, *so = sdo + OWN, *ring = O_IN_RING ? so : so + OWN;
+  Shared& s = *reinterpret_cast<Shared*>(ring + STAGES * TILE);
   const AttnCall& C = P.c;
-  if (!begin(s, P, C.heads_q, C.causal, STAGES, 256, 512)) return;
+  if (!in_place(smem, C.seqs.status)) return;
+  // The kernel before it may be the one that writes zeros to the other sequences' rows, which runs beside this one (it has begun, so
+  // all before it is done); the wait at the end makes sure that this one does not end first.  The dK, dV kernel's CTAs may come as
+  // soon as the last ones of this grid have begun.
+  pdl_trigger();
+  begin(s, P, STAGES, WARPS, WARPS, 4 * TN);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int head = (int)(blockIdx.x % (unsigned)C.heads_q), first = s.first, len = s.len, t0 = s.t0;
-  const int end_col = C.causal ? min(len, t0 + 128) : len, tiles = (end_col + 127) / 128;
-  const uint32_t ts = s.tmem, tdp = s.tmem + 256, tdq = s.tmem + 384;
+  const uint32_t ts = s.tmem, tdp = ts + 2 * TN, tdq = ts + 3 * TN;
   volatile int* ab = &s.abort_flag;
   int32_t* status = C.seqs.status;
+  auto tiles_of = [&](const Item& it) { return ((C.causal ? min(it.len, it.t0 + 128) : it.len) + TN - 1) / TN; };
 
-  if (warp == 9) {
-    if (elect_one()) {
-      mbar_expect_tx(&s.own, 2 * TILE_BYTES);
-      load_tile<DC>(sq, &mq, head, first + t0, &s.own);
-      load_tile<DC>(sdo, &mdo, head, first + t0, &s.own);
-      Ring r;
-      uint32_t filled = 0;
-      const int kv = head / C.group;
-      for (int j = 0; j < tiles; ++j) {
-        if (!mbar_wait(&s.empty[r.stage], r.phase ^ 1u, ab, status)) break;
-        if (P.stall_once && blockIdx.x == 0 && j == 0) { r.next(STAGES); continue; }
-        mbar_expect_tx(&s.full[r.stage], 2 * TILE_BYTES);
-        uint8_t* to = ring + r.stage * 2 * TILE_BYTES;
-        load_tile<DC>(to, &mk, kv, first + j * 128, &s.full[r.stage]);
-        load_tile<DC>(to + TILE_BYTES, &mv, kv, first + j * 128, &s.full[r.stage]);
-        r.next(STAGES);
-        ++filled;
+  if (warp == WARPS + 1) {
+    Ring r;
+    Item it;
+    uint32_t own = 0;
+    for (int n = 0; take_item(s, P, n, C.heads_q, C.causal, it); ++n) {
+      bool ok = warp_wait(&s.own_empty, (n & 1) ^ 1, ab, status);
+      if (!ok) break;
+      const int token = it.first + it.t0;
+      if (elect_one()) {
+        mbar_expect_tx(&s.own_full, (O_IN_RING ? 2 : 3) * OWN);
+        load_tile<DC, 128>(sq, &mq, it.head, token, &s.own_full);
+        load_tile<DC, 128>(sdo, &mdo, it.head, token, &s.own_full);
+        if (!O_IN_RING) load_tile<DC, 128>(so, &mo, it.head, token, &s.own_full);
       }
-      if (*ab) {
-        mbar_wait(&s.own, 0, ab, status);
-        drain_loads(s.full, STAGES, r.stage, r.phase, filled, ab, status);
+      ++own;
+      const int tiles = tiles_of(it), kv = it.head / C.group;
+      const bool stall = P.stall_once && blockIdx.x == 0 && n == 0;
+      for (int i = 0; i < 2 * tiles && ok; ++i) {
+        ok = fill<DC, TN>(s, r, STAGES, ring, (i & 1) ? &mv : &mk, kv, it.first + (i >> 1) * TN, stall && i == 0, status);
+        // behind the first two tiles, which the first products need
+        if (O_IN_RING && i == 1) ok = ok && fill<DC, TN>(s, r, STAGES, ring, &mo, it.head, token, false, status);
       }
+      if (!ok) break;
     }
-  } else if (warp == 8) {
+    if (lane == 0) drain(s, r, STAGES, own, status);
+  } else if (warp == WARPS) {
     const bool leader = elect_one();
-    bool ok = warp_wait(&s.own, 0, ab, status);
-    Ring load, use;
-    auto scores = [&](int j) {           // waits for tile j and multiplies it with Q
-      ok = warp_wait(&s.full[load.stage], load.phase, ab, status);
-      if (!ok) return;
-      uint8_t* at = ring + load.stage * 2 * TILE_BYTES;
-      if (len - j * 128 < 128) {
-        zero_rows<DC>(at, len - j * 128, lane);
-        zero_rows<DC>(at + TILE_BYTES, len - j * 128, lane);
-        fence_async_smem();
-        __syncwarp();
-      }
-      tc_fence_after();
-      if (leader) {
-        product_tiles<DC>(ts + (j & 1) * 128, smem_u32(sq), smem_u32(at));
-        umma_commit(&s.scores[j & 1]);
-      }
-    };
-    auto dscores = [&]() {
-      if (leader) {
-        product_tiles<DC>(tdp, smem_u32(sdo), smem_u32(ring + load.stage * 2 * TILE_BYTES + TILE_BYTES));
-        umma_commit(&s.dscores);
-      }
-    };
-    if (ok) scores(0);
-    if (ok) dscores();
-    for (int j = 0; j < tiles && ok; ++j) {
-      if (j + 1 < tiles) {
-        load.next(STAGES);
-        scores(j + 1);
-        if (!ok) break;
-      }
-      ok = warp_wait(&s.ready[0], j & 1, ab, status);
-      if (!ok) break;
-      tc_fence_after();
-      if (j + 1 < tiles) dscores();
-      if (leader) {
-        product_rows<DC>(tdq, ts + (j & 1) * 128, 64, smem_u32(ring + use.stage * 2 * TILE_BYTES), j != 0);
-        umma_commit(&s.empty[use.stage]);
-      }
-      use.next(STAGES);
-    }
-    if (leader) {
-      if (ok) umma_commit(&s.done);
-      else drain_products(&s.drain, ab, status);
-    }
-  } else {
-    const int row = t0 + (warp & 3) * 32 + lane, part = warp >> 2;       // columns part * 64 ..
-    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const float c = C.scale * ATTN_LOG2E;
-    float lse = 0.f, delta = 0.f;
-    if (row < len) {
-      const int64_t at = (int64_t)head * C.seqs.total + first + row;
-      lse = C.lse[at] * ATTN_LOG2E;
-      delta = C.delta[at];
-    }
-    const uint64_t c2 = pack2(c, c), n2 = pack2(-lse, -lse), d2 = pack2(-delta, -delta);
+    Ring r;
+    Item it;
+    uint32_t made = 0;                   // dS tiles so far
+    int score = 0;                       // score tiles so far
     bool ok = true;
-    for (int j = 0; j < tiles; ++j) {
-      ok = warp_wait(&s.scores[j & 1], (j >> 1) & 1, ab, status);
+    for (int n = 0; ok && get_item(s, n, status, it); ++n) {
+      const int tiles = tiles_of(it);
+      ok = warp_wait(&s.own_full, n & 1, ab, status);
       if (!ok) break;
-      tc_fence_after();
-      const uint32_t at = ts + lanes + (j & 1) * 128 + part * 64;
-      uint32_t a[64];
-      tmem_ld64(at, a);
-#pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        float e0, e1;
-        unpack2(fma2(pack2(__uint_as_float(a[2 * i]), __uint_as_float(a[2 * i + 1])), c2, n2), e0, e1);
-        a[2 * i] = __float_as_uint(attn_exp2(e0));
-        a[2 * i + 1] = __float_as_uint(attn_exp2(e1));
+      int k_now = 0, k_next = 0, v_next = 0;         // ring places of this tile's K, and of the next one's K and V
+      // waits for K and V of tile j and multiplies K with Q
+      auto scores = [&](int j) {
+        const int have = it.len - j * TN;
+        for (int x = 0; x < 2 && ok; ++x) {
+          ok = warp_wait(&s.full[r.stage], r.phase, ab, status);
+          if (ok && have < TN) zero_rows<DC, TN>(ring + r.stage * TILE, have, lane);
+          (x == 0 ? k_next : v_next) = r.stage;
+          r.next(STAGES);
+        }
+        if (!ok) return;
+        if (have < TN) {
+          fence_async_smem();
+          __syncwarp();
+        }
+        tc_fence_after();
+        if (leader) {
+          product_tiles<DC, TN>(ts + (score & 1) * TN, smem_u32(sq), smem_u32(ring + k_next * TILE));
+          umma_commit(&s.scores[score & 1]);
+        }
+        ++score;
+      };
+      auto dscores = [&](bool last) {
+        if (leader) {
+          product_tiles<DC, TN>(tdp, smem_u32(sdo), smem_u32(ring + v_next * TILE));
+          umma_commit(&s.dscores);
+          umma_commit(&s.empty[v_next]);
+          if (last) umma_commit(&s.own_empty);
+        }
+      };
+      scores(0);
+      if (!ok) break;
+      dscores(tiles == 1);
+      if (O_IN_RING) {
+        // O's place is given back when the other warps have read it
+        ok = warp_wait(&s.o_read, n & 1, ab, status);
+        if (!ok) break;
+        if (leader) mbar_arrive(&s.empty[r.stage]);
+        r.next(STAGES);
       }
-      ok = warp_wait(&s.dscores, j & 1, ab, status);
-      if (!ok) break;
-      tc_fence_after();
-      uint32_t o[32];
-      const int see = min(128, (C.causal ? min(len, row + 1) : len) - j * 128) - part * 64;
-      const bool whole = !__any_sync(0xffffffffu, see < 64);
-      {
-        uint32_t b[64];
-        tmem_ld64(tdp + lanes + part * 64, b);
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          float s0, s1;
-          unpack2(mul2(pack2(__uint_as_float(a[2 * i]), __uint_as_float(a[2 * i + 1])),
-                       add2(pack2(__uint_as_float(b[2 * i]), __uint_as_float(b[2 * i + 1])), d2)), s0, s1);
-          if (!whole) {
-            s0 = 2 * i < see ? s0 : 0.f;
-            s1 = 2 * i + 1 < see ? s1 : 0.f;
-          }
-          o[i] = pack_bf16(s0, s1);
+      for (int j = 0; j < tiles; ++j, ++made) {
+        k_now = k_next;
+        if (j + 1 < tiles) {
+          scores(j + 1);
+          if (!ok) break;
+        }
+        if (j == 0) ok = warp_wait(&s.acc_empty, (n & 1) ^ 1, ab, status);
+        ok = ok && warp_wait(&s.ready[0], made & 1, ab, status);
+        if (!ok) break;
+        tc_fence_after();
+        if (j + 1 < tiles) dscores(j + 2 == tiles);
+        if (leader) {
+          product_rows<DC, TN, 0, TN / 16>(tdq, ts + (made & 1) * TN, 64, smem_u32(ring + k_now * TILE), j != 0);
+          umma_commit(&s.empty[k_now]);
+          if (j == tiles - 1) umma_commit(&s.done);
         }
       }
-      tmem_st32(at, o);
-      tmem_wait_st();
-      tc_fence_before();
-      mbar_arrive(&s.ready[0]);
     }
-    ok = ok && warp_wait(&s.done, 0, ab, status);
-    if (ok && part < DC) {
-      // each half of the warps stores 64 columns (all of them where there are no more)
+    if (leader && *ab) drain_products(&s.drain, ab, status);
+  } else {
+    const int part = warp >> 2;          // columns part * 64 ..
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const float c = C.scale * ATTN_LOG2E;
+    const uint64_t c2 = pack2(c, c);
+    Item it;
+    uint32_t made = 0;
+    Ring r;                              // the loads, to find O among them
+    bool ok = true;
+    for (int n = 0; ok && get_item(s, n, status, it); ++n) {
+      const int tiles = tiles_of(it), in = (warp & 3) * 32 + lane, row = it.t0 + in;
+      const int64_t at_row = (int64_t)it.head * C.seqs.total + it.first + row;
+      const float lse = row < it.len ? __ldcg(C.lse + at_row) * ATTN_LOG2E : 0.f;
+      ok = warp_wait(&s.own_full, n & 1, ab, status);
+      if (!ok) break;
+      const uint8_t* o_tile = so;
+      if (O_IN_RING) {
+        r.next(STAGES);
+        r.next(STAGES);
+        ok = warp_wait(&s.full[r.stage], r.phase, ab, status);
+        if (!ok) break;
+        o_tile = ring + r.stage * TILE;
+        r.next(STAGES);
+        for (int i = 2; i < 2 * tiles; ++i) r.next(STAGES);
+      }
+      // by all warps that need it; the dK, dV kernel reads it
+      const float delta = row_dot<DC>(sdo, o_tile, in);
+      if (O_IN_RING) warp_arrive(&s.o_read);
+      warp_arrive(&s.own_empty);
+      if (part == 0 && row < it.len) C.delta[at_row] = delta;
+      const uint64_t n2 = pack2(-lse, -lse), d2 = pack2(-delta, -delta);
+      for (int j = 0; j < tiles; ++j, ++made) {
+        ok = warp_wait(&s.scores[made & 1], (made >> 1) & 1, ab, status);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t at = ts + lanes + (made & 1) * TN + part * 64;
+        uint32_t a[64];
+        tmem_ld64(at, a);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          float e0, e1;
+          unpack2(fma2(pack2(__uint_as_float(a[2 * i]), __uint_as_float(a[2 * i + 1])), c2, n2), e0, e1);
+          a[2 * i] = __float_as_uint(attn_exp2(e0));
+          a[2 * i + 1] = __float_as_uint(attn_exp2(e1));
+        }
+        ok = warp_wait(&s.dscores, made & 1, ab, status);
+        if (!ok) break;
+        tc_fence_after();
+        uint32_t o[32];
+        const int see = min(TN, (C.causal ? min(it.len, row + 1) : it.len) - j * TN) - part * 64;
+        const bool whole = !__any_sync(0xffffffffu, see < 64);
+        {
+          uint32_t b[64];
+          tmem_ld64(tdp + lanes + part * 64, b);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            float s0, s1;
+            unpack2(mul2(pack2(__uint_as_float(a[2 * i]), __uint_as_float(a[2 * i + 1])),
+                         add2(pack2(__uint_as_float(b[2 * i]), __uint_as_float(b[2 * i + 1])), d2)), s0, s1);
+            if (!whole) {
+              s0 = 2 * i < see ? s0 : 0.f;
+              s1 = 2 * i + 1 < see ? s1 : 0.f;
+            }
+            o[i] = pack_bf16(s0, s1);
+          }
+        }
+        tmem_st32(at, o);
+        tmem_wait_st();
+        tc_fence_before();
+        warp_arrive(&s.ready[0]);
+      }
+      ok = ok && warp_wait(&s.done, n & 1, ab, status);
+      if (!ok) break;
+      // a warp stores 64 columns
+      static_assert(WARPS == 4 * DC, "every column has a warp");
       tc_fence_after();
-      __nv_bfloat16* o = (__nv_bfloat16*)const_cast<void*>(C.dq.p) + (int64_t)(first + row) * C.dq.token + (int64_t)head * C.dq.head;
-      store_row<1>(tdq + lanes + part * 64, o + part * 64, C.dim - part * 64, row < len, C.scale);
+      Strided x = C.dq;
+      x.p = (const __nv_bfloat16*)x.p + part * 64;
+      const int warp_row = it.t0 + (warp & 3) * 32;
+      store_rows<1>(tdq + lanes + part * 64, x, (int64_t)it.first + warp_row, it.head, C.dim - part * 64, it.len - warp_row, C.scale);
+      tc_fence_before();
+      warp_arrive(&s.acc_empty);
     }
   }
-  end(s, 512);
+  pdl_wait();
+  end(s, P, 4 * TN);
 }
 
 // Rows are keys.  TMEM: S^T (P^T replaces it), dP^T (dS^T replaces it), dV, dK.  The products of tile i + 1's scores are issued
 // between those of tile i: S^T(i + 1) behind dV(i), dP^T(i + 1) behind dK(i), so that the tensor pipe works while the other
 // warps do exponentials.
 template <int DC>
-__global__ void __launch_bounds__(BWD_THREADS, 1)
+__global__ void __launch_bounds__(BWD_THREADS<DC>, BWD_CTAS<DC>)
 attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mdo, const __grid_constant__ CUtensorMap mk,
                 const __grid_constant__ CUtensorMap mv, const __grid_constant__ UmmaCall P) {
-  constexpr int STAGES = 2, TILE_BYTES = DC * CHUNK;
-  extern __shared__ uint8_t raw[];
-  __shared__ Shared s;
-  __shared__ __align__(16) float s_rows[8][2][128];      // each warp's own: lse and delta of its 64 queries, two items
-  uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
-  uint8_t *sk = smem, *sv = smem + TILE_BYTES, *ring = smem + 2 * TILE_BYTES;       // a stage: Q, dO
+  constexpr int STAGES = BWD_STAGES<DC>, TN = TN_OF<DC>, WARPS = BWD_WARPS<DC>, OWN = DC * CHUNK<128>, TILE = DC * CHUNK<TN>;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  uint8_t *sk = smem, *sv = sk + OWN, *ring = sv + OWN;
+  float* s_rows = reinterpret_cast<float*>(ring + STAGES * TILE);    // [2 steps][TN / 64 parts]: lse and delta of 64 queries
+  Shared& s = *reinterpret_cast<Shared*>(s_rows + 2 * (TN / 64) * 128);
   const AttnCall& C = P.c;
-  if (!begin(s, P, C.heads_kv, false, STAGES, 256, 512)) return;
+  if (!in_place(smem, C.seqs.status)) return;
+  begin(s, P, STAGES, WARPS, 0, 4 * TN);
+  pdl_wait();                            // delta comes from the dQ kernel
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int kv = (int)(blockIdx.x % (unsigned)C.heads_kv), first = s.first, len = s.len, t0 = s.t0;
-  const int q0 = C.causal ? t0 / 128 : 0, per_head = (len + 127) / 128 - q0, items = per_head * C.group;
-  const uint32_t ts = s.tmem, tdp = s.tmem + 128, tdv = s.tmem + 256, tdk = s.tmem + 384;
+  const uint32_t ts = s.tmem, tdp = ts + TN, tdv = ts + 2 * TN, tdk = tdv + 64 * DC;
   volatile int* ab = &s.abort_flag;
   int32_t* status = C.seqs.status;
-  auto head_of = [&](int i) { return kv * C.group + i / per_head; };
-  auto row_of = [&](int i) { return (q0 + i % per_head) * 128; };          // first query of item i
+  // An item's steps: the query tiles from the first that sees a key of this tile, for one head of the group after the other.
+  auto first_tile = [&](const Item& it) { return C.causal ? it.t0 / TN : 0; };
+  auto per_head = [&](const Item& it) { return (it.len + TN - 1) / TN - first_tile(it); };
+  struct Step { int head, row; };
+  auto step_of = [&](const Item& it, int i, int per) { return Step{it.head * C.group + i / per, (first_tile(it) + i % per) * TN}; };
 
-  if (warp == 9) {
-    if (elect_one()) {
-      mbar_expect_tx(&s.own, 2 * TILE_BYTES);
-      load_tile<DC>(sk, &mk, kv, first + t0, &s.own);
-      load_tile<DC>(sv, &mv, kv, first + t0, &s.own);
-      Ring r;
-      uint32_t filled = 0;
-      for (int i = 0; i < items; ++i) {
-        if (!mbar_wait(&s.empty[r.stage], r.phase ^ 1u, ab, status)) break;
-        if (P.stall_once && blockIdx.x == 0 && i == 0) { r.next(STAGES); continue; }
-        mbar_expect_tx(&s.full[r.stage], 2 * TILE_BYTES);
-        uint8_t* to = ring + r.stage * 2 * TILE_BYTES;
-        load_tile<DC>(to, &mq, head_of(i), first + row_of(i), &s.full[r.stage]);
-        load_tile<DC>(to + TILE_BYTES, &mdo, head_of(i), first + row_of(i), &s.full[r.stage]);
-        r.next(STAGES);
-        ++filled;
+  if (warp == WARPS + 1) {
+    Ring r;
+    Item it;
+    uint32_t own = 0;
+    for (int n = 0; take_item(s, P, n, C.heads_kv, false, it); ++n) {
+      bool ok = warp_wait(&s.own_empty, (n & 1) ^ 1, ab, status);
+      if (!ok) break;
+      if (elect_one()) {
+        mbar_expect_tx(&s.own_full, 2 * OWN);
+        load_tile<DC, 128>(sk, &mk, it.head, it.first + it.t0, &s.own_full);
+        load_tile<DC, 128>(sv, &mv, it.head, it.first + it.t0, &s.own_full);
       }
-      if (*ab) {
-        mbar_wait(&s.own, 0, ab, status);
-        drain_loads(s.full, STAGES, r.stage, r.phase, filled, ab, status);
+      ++own;
+      const int per = per_head(it), steps = per * C.group;
+      const bool stall = P.stall_once && blockIdx.x == 0 && n == 0;
+      for (int i = 0; i < 2 * steps && ok; ++i) {
+        const Step st = step_of(it, i >> 1, per);
+        ok = fill<DC, TN>(s, r, STAGES, ring, (i & 1) ? &mdo : &mq, st.head, it.first + st.row, stall && i == 0, status);
       }
+      if (!ok) break;
     }
-  } else if (warp == 8) {
+    if (lane == 0) drain(s, r, STAGES, own, status);
+  } else if (warp == WARPS) {
     const bool leader = elect_one();
-    bool ok = warp_wait(&s.own, 0, ab, status);
-    Ring load, use;
-    auto scores = [&](int i) {
-      ok = warp_wait(&s.full[load.stage], load.phase, ab, status);
-      if (!ok) return;
-      uint8_t* at = ring + load.stage * 2 * TILE_BYTES;
-      const int have = len - row_of(i);
-      if (have < 128) {
-        zero_rows<DC>(at, have, lane);
-        zero_rows<DC>(at + TILE_BYTES, have, lane);
-        fence_async_smem();
-        __syncwarp();
-      }
-      tc_fence_after();
-      if (leader) {
-        product_tiles<DC>(ts, smem_u32(sk), smem_u32(at));
-        umma_commit(&s.scores[0]);
-      }
-    };
-    auto dscores = [&]() {
-      if (leader) {
-        product_tiles<DC>(tdp, smem_u32(sv), smem_u32(ring + load.stage * 2 * TILE_BYTES + TILE_BYTES));
-        umma_commit(&s.dscores);
-      }
-    };
-    if (ok) scores(0);
-    if (ok) dscores();
-    for (int i = 0; i < items && ok; ++i) {
-      const uint32_t at = smem_u32(ring + use.stage * 2 * TILE_BYTES);
-      ok = warp_wait(&s.ready[0], i & 1, ab, status);
+    Ring r;
+    Item it;
+    uint32_t made = 0;
+    bool ok = true;
+    for (int n = 0; ok && get_item(s, n, status, it); ++n) {
+      const int per = per_head(it), steps = per * C.group;
+      ok = warp_wait(&s.own_full, n & 1, ab, status);
       if (!ok) break;
-      tc_fence_after();
-      if (leader) product_rows<DC>(tdv, ts, 64, at + TILE_BYTES, i != 0);
-      if (i + 1 < items) {
-        load.next(STAGES);
-        scores(i + 1);
+      int q_next = 0, g_next = 0;        // ring places of the next step's Q and dO
+      auto scores = [&](int i) {
+        const int have = it.len - step_of(it, i, per).row;
+        for (int x = 0; x < 2 && ok; ++x) {
+          ok = warp_wait(&s.full[r.stage], r.phase, ab, status);
+          if (ok && have < TN) zero_rows<DC, TN>(ring + r.stage * TILE, have, lane);
+          (x == 0 ? q_next : g_next) = r.stage;
+          r.next(STAGES);
+        }
+        if (!ok) return;
+        if (have < TN) {
+          fence_async_smem();
+          __syncwarp();
+        }
+        tc_fence_after();
+        if (leader) {
+          product_tiles<DC, TN>(ts, smem_u32(sk), smem_u32(ring + q_next * TILE));
+          umma_commit(&s.scores[0]);
+        }
+      };
+      auto dscores = [&](int i) {
+        if (leader) {
+          product_tiles<DC, TN>(tdp, smem_u32(sv), smem_u32(ring + g_next * TILE));
+          umma_commit(&s.dscores);
+          if (i == steps - 1) umma_commit(&s.own_empty);
+        }
+      };
+      scores(0);
+      if (!ok) break;
+      dscores(0);
+      for (int i = 0; i < steps; ++i, ++made) {
+        if (i == 0) ok = warp_wait(&s.acc_empty, (n & 1) ^ 1, ab, status);
+        ok = ok && warp_wait(&s.ready[0], made & 1, ab, status);
         if (!ok) break;
+        tc_fence_after();
+        const int q = q_next, g = g_next;
+        if (leader) {
+          product_rows<DC, TN, 0, TN / 16>(tdv, ts, 64, smem_u32(ring + g * TILE), i != 0);
+          umma_commit(&s.empty[g]);
+        }
+        if (i + 1 < steps) {
+          scores(i + 1);
+          if (!ok) break;
+        }
+        ok = warp_wait(&s.ready[1], made & 1, ab, status);
+        if (!ok) break;
+        tc_fence_after();
+        if (leader) {
+          product_rows<DC, TN, 0, TN / 16>(tdk, tdp, 64, smem_u32(ring + q * TILE), i != 0);
+          umma_commit(&s.empty[q]);
+          if (i == steps - 1) umma_commit(&s.done);
+        }
+        if (i + 1 < steps) dscores(i + 1);
       }
-      ok = warp_wait(&s.ready[1], i & 1, ab, status);
-      if (!ok) break;
-      tc_fence_after();
-      if (leader) {
-        product_rows<DC>(tdk, tdp, 64, at, i != 0);
-        umma_commit(&s.empty[use.stage]);
-      }
-      use.next(STAGES);
-      if (i + 1 < items) dscores();
     }
-    if (leader) {
-      if (ok) umma_commit(&s.done);
-      else drain_products(&s.drain, ab, status);
-    }
+    if (leader && *ab) drain_products(&s.drain, ab, status);
   } else {
-    const int row = t0 + (warp & 3) * 32 + lane, part = warp >> 2;
+    const int part = warp >> 2;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const float c = C.scale * ATTN_LOG2E;
     const uint64_t c2 = pack2(c, c);
-    // a lane's two queries of an item: their lse (in units of log 2) and delta, negative
-    auto fetch = [&](int i) -> float4 {
-      const int t = row_of(i) + part * 64 + 2 * lane;
-      const int64_t at = (int64_t)head_of(i) * C.seqs.total + first + t;
-      float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (t < len) { f.x = -C.lse[at] * ATTN_LOG2E; f.z = -C.delta[at]; }
-      if (t + 1 < len) { f.y = -C.lse[at + 1] * ATTN_LOG2E; f.w = -C.delta[at + 1]; }
-      return f;
-    };
-    auto keep = [&](int i, float4 f) {
-      float* at = s_rows[warp][i & 1] + 2 * lane;
-      *reinterpret_cast<float2*>(at) = make_float2(f.x, f.y);
-      *reinterpret_cast<float2*>(at + 64) = make_float2(f.z, f.w);
-      __syncwarp();
-    };
-    keep(0, fetch(0));
+    Item it;
+    uint32_t made = 0;
     bool ok = true;
-    for (int i = 0; i < items; ++i) {
-      const float4 ahead = i + 1 < items ? fetch(i + 1) : make_float4(0.f, 0.f, 0.f, 0.f);
-      ok = warp_wait(&s.scores[0], i & 1, ab, status);
-      if (!ok) break;
-      tc_fence_after();
-      const int base = row_of(i) + part * 64;        // first query of this warp's columns
-      const bool cut = len - base < 64 || (C.causal && base < t0 + 128);
-      const int lo = C.causal ? row - base : 0, hi = len - base;         // the columns that look at this key
-      uint32_t a[64];
-      tmem_ld64(ts + lanes + part * 64, a);
-      uint32_t o[32];
-#pragma unroll
-      for (int e = 0; e < 32; e += 2) {
-        const float4 n = *reinterpret_cast<const float4*>(&s_rows[warp][i & 1][2 * e]);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int x = 2 * (e + h);
-          float e0, e1;
-          unpack2(fma2(pack2(__uint_as_float(a[x]), __uint_as_float(a[x + 1])), c2, h == 0 ? pack2(n.x, n.y) : pack2(n.z, n.w)), e0, e1);
-          e0 = attn_exp2(e0);
-          e1 = attn_exp2(e1);
-          if (cut) {
-            e0 = x >= lo && x < hi ? e0 : 0.f;
-            e1 = x + 1 >= lo && x + 1 < hi ? e1 : 0.f;
-          }
-          a[x] = __float_as_uint(e0);
-          a[x + 1] = __float_as_uint(e1);
-          o[e + h] = pack_bf16(e0, e1);
-        }
-      }
-      tmem_st32(ts + lanes + part * 64, o);
-      tmem_wait_st();
-      tc_fence_before();
-      mbar_arrive(&s.ready[0]);
-      ok = warp_wait(&s.dscores, i & 1, ab, status);
-      if (!ok) break;
-      tc_fence_after();
-      {
-        uint32_t b[64];
-        tmem_ld64(tdp + lanes + part * 64, b);
+    for (int n = 0; ok && get_item(s, n, status, it); ++n) {
+      const int per = per_head(it), steps = per * C.group, warp_row = it.t0 + (warp & 3) * 32, row = warp_row + lane;
+      // Negative lse (in units of log 2) and delta of a step's 64 queries, for the four warps of this half: a warp brings 16 of them.
+      auto fetch = [&](int i) -> float {
+        const Step st = step_of(it, i, per);
+        const int t = st.row + part * 64 + (warp & 3) * 16 + (lane & 15);
+        const int64_t at = (int64_t)st.head * C.seqs.total + it.first + t;
+        return t >= it.len ? 0.f : lane < 16 ? -C.lse[at] * ATTN_LOG2E : -C.delta[at];
+      };
+      auto keep = [&](uint32_t k, float f) {
+        s_rows[((k & 1) * (TN / 64) + part) * 128 + (lane >> 4) * 64 + (warp & 3) * 16 + (lane & 15)] = f;
+        warp_arrive(&s.rows_full[part][k & 1]);
+      };
+      keep(made, fetch(0));
+      for (int i = 0; i < steps; ++i, ++made) {
+        const float ahead = i + 1 < steps ? fetch(i + 1) : 0.f;
+        const float* mine = s_rows + ((made & 1) * (TN / 64) + part) * 128;
+        ok = warp_wait(&s.rows_full[part][made & 1], (made >> 1) & 1, ab, status) && warp_wait(&s.scores[0], made & 1, ab, status);
+        if (!ok) break;
+        tc_fence_after();
+        const int base = step_of(it, i, per).row + part * 64;      // first query of this warp's columns
+        const bool cut = it.len - base < 64 || (C.causal && base < it.t0 + 128);
+        const int lo = C.causal ? row - base : 0, hi = it.len - base;    // the columns that look at this key
+        uint32_t a[64];
+        tmem_ld64(ts + lanes + part * 64, a);
+        uint32_t o[32];
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
-          const float4 n = *reinterpret_cast<const float4*>(&s_rows[warp][i & 1][64 + 2 * e]);
+          const float4 f = *reinterpret_cast<const float4*>(mine + 2 * e);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const int x = 2 * (e + h);
-            float s0, s1;
-            unpack2(mul2(pack2(__uint_as_float(a[x]), __uint_as_float(a[x + 1])),
-                         add2(pack2(__uint_as_float(b[x]), __uint_as_float(b[x + 1])), h == 0 ? pack2(n.x, n.y) : pack2(n.z, n.w))), s0, s1);
-            o[e + h] = pack_bf16(s0, s1);
+            float e0, e1;
+            unpack2(fma2(pack2(__uint_as_float(a[x]), __uint_as_float(a[x + 1])), c2, h == 0 ? pack2(f.x, f.y) : pack2(f.z, f.w)), e0, e1);
+            e0 = attn_exp2(e0);
+            e1 = attn_exp2(e1);
+            if (cut) {
+              e0 = x >= lo && x < hi ? e0 : 0.f;
+              e1 = x + 1 >= lo && x + 1 < hi ? e1 : 0.f;
+            }
+            a[x] = __float_as_uint(e0);
+            a[x + 1] = __float_as_uint(e1);
+            o[e + h] = pack_bf16(e0, e1);
           }
         }
+        tmem_st32(ts + lanes + part * 64, o);
+        tmem_wait_st();
+        tc_fence_before();
+        warp_arrive(&s.ready[0]);
+        ok = warp_wait(&s.dscores, made & 1, ab, status);
+        if (!ok) break;
+        tc_fence_after();
+        {
+          uint32_t b[64];
+          tmem_ld64(tdp + lanes + part * 64, b);
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) {
+            const float4 f = *reinterpret_cast<const float4*>(mine + 64 + 2 * e);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const int x = 2 * (e + h);
+              float s0, s1;
+              unpack2(mul2(pack2(__uint_as_float(a[x]), __uint_as_float(a[x + 1])),
+                           add2(pack2(__uint_as_float(b[x]), __uint_as_float(b[x + 1])), h == 0 ? pack2(f.x, f.y) : pack2(f.z, f.w))), s0, s1);
+              o[e + h] = pack_bf16(s0, s1);
+            }
+          }
+        }
+        tmem_st32(tdp + lanes + part * 64, o);
+        tmem_wait_st();
+        tc_fence_before();
+        warp_arrive(&s.ready[1]);
+        if (i + 1 < steps) keep(made + 1, ahead);
       }
-      tmem_st32(tdp + lanes + part * 64, o);
-      tmem_wait_st();
-      tc_fence_before();
-      mbar_arrive(&s.ready[1]);
-      if (i + 1 < items) keep(i + 1, ahead);
-    }
-    ok = ok && warp_wait(&s.done, 0, ab, status);
-    if (ok) {
-      // one half of the warps stores dV, the other dK
+      ok = ok && warp_wait(&s.done, n & 1, ab, status);
+      if (!ok) break;
+      // with eight warps one half stores dV, the other dK
       tc_fence_after();
-      const Strided& x = part == 0 ? C.dv : C.dk;
-      __nv_bfloat16* o = (__nv_bfloat16*)const_cast<void*>(x.p) + (int64_t)(first + row) * x.token + (int64_t)kv * x.head;
-      store_row<DC>((part == 0 ? tdv : tdk) + lanes, o, C.dim, row < len, part == 0 ? 1.0f : C.scale);
+      auto store = [&](const Strided& x, uint32_t from, float f) {
+        store_rows<DC>(from + lanes, x, (int64_t)it.first + warp_row, it.head, C.dim, it.len - warp_row, f);
+      };
+      if (WARPS == 4 || part == 0) store(C.dv, tdv, 1.0f);
+      if (WARPS == 4 || part == 1) store(C.dk, tdk, C.scale);
+      tc_fence_before();
+      warp_arrive(&s.acc_empty);
     }
   }
-  end(s, 512);
+  end(s, P, 4 * TN);
 }
 
 // --------------------------------------------------------------------------------------------- host
-// [total, heads, dim] with a box of 64 columns of one head of 128 tokens
-bool attn_map(CUtensorMap* m, const Strided& x, int heads, int dim, int total) {
+// [total, heads, dim] with a box of 64 columns of one head of `rows` tokens
+bool attn_map(CUtensorMap* m, const Strided& x, int heads, int dim, int total, int rows) {
   const uint64_t dims[3] = {(uint64_t)dim, (uint64_t)heads, (uint64_t)total};
   // a stride along an extent of one is never used, but has to be a valid one
   const uint64_t strides[2] = {heads > 1 ? (uint64_t)x.head * 2 : 16, total > 1 ? (uint64_t)x.token * 2 : 16};
-  const uint32_t box[3] = {64, 1, 128};
+  const uint32_t box[3] = {64, 1, (uint32_t)rows};
   return make_map(m, x.p, 3, dims, strides, box);
 }
 bool addressable(const Strided& x, int heads, int total) {
   return ((uintptr_t)x.p & 15) == 0 && (total == 1 || (x.token % 8 == 0 && x.token > 0)) && (heads == 1 || (x.head % 8 == 0 && x.head > 0)) &&
          x.token < (1ll << 36) && x.head < (1ll << 36);
 }
-template <typename K, typename... M>
-cudaError_t run(K kernel, int tiles_of_smem, int threads, long grid, const Attn* a, const AttnCall& c, int dc, cudaStream_t st, const M&... maps) {
-  if (grid > 0x7fffffffl) return cudaErrorInvalidValue;
-  const int smem = tiles_of_smem * dc * CHUNK + 1024;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+template <typename... KArgs, typename... M>
+cudaError_t run(void (*kernel)(KArgs...), bool after, int which, int bytes, int threads, int ctas, long tiles, const Attn* a,
+                const AttnCall& c, cudaStream_t st, const M&... maps) {
+  if (tiles + (long)ctas * a->num_sms > 0x7fffffffl) return cudaErrorInvalidValue;       // the counter's range
+  const long grid = tiles < (long)ctas * a->num_sms ? tiles : (long)ctas * a->num_sms;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes + (int)sizeof(Shared));
   if (e != cudaSuccess) return e;
-  const UmmaCall P = {c, a->wait_limit_ns, a->stall_once};
-  kernel<<<(unsigned)grid, threads, smem, st>>>(maps..., P);
-  return cudaGetLastError();
+  const UmmaCall P = {c, a->next + 2 * which, a->wait_limit_ns, a->stall_once};
+  return launch_maybe_after(after, kernel, dim3((unsigned)grid), dim3(threads), bytes + sizeof(Shared), st, maps..., P);
+}
+template <int DC>
+cudaError_t backward(const Attn* a, const AttnCall& c, bool after, cudaStream_t st) {
+  constexpr int TN = TN_OF<DC>;
+  const int total = c.seqs.total, hq = c.heads_q, hk = c.heads_kv, d = c.dim;
+  CUtensorMap q, g, o, k, v, qt, gt, kt, vt;         // tiles of 128 rows, and of TN
+  if (!attn_map(&q, c.q, hq, d, total, 128) || !attn_map(&g, c.d_o, hq, d, total, 128) || !attn_map(&o, c.o, hq, d, total, 128) ||
+      !attn_map(&kt, c.k, hk, d, total, TN) || !attn_map(&vt, c.v, hk, d, total, TN) || !attn_map(&qt, c.q, hq, d, total, TN) ||
+      !attn_map(&gt, c.d_o, hq, d, total, TN) || !attn_map(&k, c.k, hk, d, total, 128) || !attn_map(&v, c.v, hk, d, total, 128))
+    return cudaErrorInvalidValue;
+  const long tiles = tile_bound(total, c.seqs.N, 128);
+  constexpr int OWN = DC * CHUNK<128>, RING = BWD_STAGES<DC> * DC * CHUNK<TN>;
+  const cudaError_t e = run(attn_dq_kernel<DC>, after, 1, (DC == 1 ? 3 : 2) * OWN + RING, BWD_THREADS<DC>, BWD_CTAS<DC>, tiles * hq, a, c, st, q,
+                            g, o, kt, vt);
+  if (e != cudaSuccess) return e;
+  return run(attn_dkv_kernel<DC>, true, 2, 2 * OWN + RING + 2 * (TN / 64) * 512, BWD_THREADS<DC>, BWD_CTAS<DC>, tiles * hk, a, c, st, qt, gt, k, v);
 }
 
 }  // namespace
@@ -732,27 +985,21 @@ bool attn_umma_ok(const Attn* a, const AttnCall& c, bool backward) {
 cudaError_t launch_attn_umma_fwd(const Attn* a, const AttnCall& c, cudaStream_t st) {
   const int total = c.seqs.total;
   CUtensorMap mq, mk, mv;
-  if (!attn_map(&mq, c.q, c.heads_q, c.dim, total) || !attn_map(&mk, c.k, c.heads_kv, c.dim, total) ||
-      !attn_map(&mv, c.v, c.heads_kv, c.dim, total))
+  if (!attn_map(&mq, c.q, c.heads_q, c.dim, total, 128) || !attn_map(&mk, c.k, c.heads_kv, c.dim, total, 128) ||
+      !attn_map(&mv, c.v, c.heads_kv, c.dim, total, 128))
     return cudaErrorInvalidValue;
-  const long grid = tile_bound(total, c.seqs.N, 128) * c.heads_q;
-  return c.dim <= 64 ? run(attn_fwd_kernel<1>, 1 + FWD_STAGES<1>, FWD_THREADS, grid, a, c, 1, st, mq, mk, mv)
-                     : run(attn_fwd_kernel<2>, 1 + FWD_STAGES<2>, FWD_THREADS, grid, a, c, 2, st, mq, mk, mv);
+  const long tiles = tile_bound(total, c.seqs.N, 128) * c.heads_q;
+  return c.dim <= 64 ? run(attn_fwd_kernel<1>, false, 0, (1 + FWD_STAGES<1>) * CHUNK<128>, FWD_THREADS, 2, tiles, a, c, st, mq, mk, mv)
+                     : run(attn_fwd_kernel<2>, false, 0, (1 + FWD_STAGES<2>) * 2 * CHUNK<128>, FWD_THREADS, 2, tiles, a, c, st, mq, mk, mv);
 }
 
 cudaError_t launch_attn_umma_bwd(const Attn* a, const AttnCall& c, cudaStream_t st) {
-  const int total = c.seqs.total;
-  CUtensorMap mq, mdo, mk, mv;
-  if (!attn_map(&mq, c.q, c.heads_q, c.dim, total) || !attn_map(&mdo, c.d_o, c.heads_q, c.dim, total) ||
-      !attn_map(&mk, c.k, c.heads_kv, c.dim, total) || !attn_map(&mv, c.v, c.heads_kv, c.dim, total))
-    return cudaErrorInvalidValue;
-  const long tiles = tile_bound(total, c.seqs.N, 128);
-  const int dc = c.dim <= 64 ? 1 : 2;
-  const cudaError_t e = dc == 1 ? run(attn_dq_kernel<1>, 6, BWD_THREADS, tiles * c.heads_q, a, c, dc, st, mq, mdo, mk, mv)
-                                : run(attn_dq_kernel<2>, 6, BWD_THREADS, tiles * c.heads_q, a, c, dc, st, mq, mdo, mk, mv);
-  if (e != cudaSuccess) return e;
-  return dc == 1 ? run(attn_dkv_kernel<1>, 6, BWD_THREADS, tiles * c.heads_kv, a, c, dc, st, mq, mdo, mk, mv)
-                 : run(attn_dkv_kernel<2>, 6, BWD_THREADS, tiles * c.heads_kv, a, c, dc, st, mq, mdo, mk, mv);
+  const bool zeros = c.seqs.alive != nullptr && !c.skip_dropped;
+  if (zeros) {
+    const cudaError_t e = launch_attn_zero(a, c, st);
+    if (e != cudaSuccess) return e;
+  }
+  return c.dim <= 64 ? backward<1>(a, c, zeros, st) : backward<2>(a, c, zeros, st);
 }
 
 }  // namespace vcas
