@@ -5,7 +5,7 @@
 // four or eight warps turn scores into probabilities, a row of TMEM being a lane's own.  Scores stay in TMEM; P and dS go back
 // there as bf16, over the scores they came from, and are the A operand of the product that follows.  tcgen05.mma of one thread run in
 // order, so a tile of scores may be overwritten by the next product as soon as the product that reads it is issued.
-//   forward    S = Q K^T,  P = exp(S - m),  O += P V; O is rescaled only where the maximum rose by more than 2^8
+//   forward    S = Q K^T,  P = exp(S - m),  O += P V; O is rescaled only where the maximum has risen by more than 2^8
 //   dQ         rows are queries: S, dP = dO V^T, dS = P (dP - delta), dQ += dS K
 //   dK, dV     rows are keys:    S^T = K Q^T, dV += P^T dO, dP^T = V dO^T, dK += dS^T Q, over all query heads of the group
 // A tile that reaches past its sequence's end holds rows of the next one (or zeros): their scores are masked, and where such rows
@@ -153,7 +153,7 @@ __device__ __forceinline__ void store_rows(uint32_t taddr, const Strided& x, int
 }
 
 // ----------------------------------------------------------------------------------------- the CTA
-constexpr int MAX_STAGES = 6;
+constexpr int MAX_STAGES = 8;
 struct Item { int first, len, t0, head, any; };      // a tile of 128 rows: its sequence, its first row in there, its head
 struct Shared {
   uint64_t full[MAX_STAGES], empty[MAX_STAGES];      // ring of the other side's tiles
@@ -163,6 +163,7 @@ struct Shared {
   uint64_t ready[2];                                 // P, dS written
   uint64_t done, acc_empty;                          // accumulators complete, and read
   uint64_t o_read, drain;
+  uint64_t added;                                    // forward: P V of a tile is in O
   uint64_t rows_full[2][2];                          // dK, dV: the queries' values, by column half and buffer
   uint32_t tmem;
   int abort_flag;                                    // mbar_wait finds the limit 20 bytes behind it
@@ -210,6 +211,7 @@ __device__ __forceinline__ void begin(Shared& s, const UmmaCall& P, int stages, 
     mbar_init(&s.done, 1);
     mbar_init(&s.acc_empty, warps);
     mbar_init(&s.o_read, warps);
+    mbar_init(&s.added, 1);
     for (int i = 0; i < 4; ++i) mbar_init(&s.rows_full[i >> 1][i & 1], 4);
     mbar_init(&s.drain, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -294,50 +296,32 @@ __device__ __forceinline__ void drain(Shared& s, const Ring& r, int stages, uint
 }
 
 // ------------------------------------------------------------------------------------------ forward
-// 2^x by the FMA pipe: x = n + f, |f| <= 1/2, n goes to the exponent, 2^f by the polynomial of degree 5 with the least largest relative
-// error there (7.5e-8, by Remez exchange).  x is at most about 8; below -127 the result is under 2^-126.
-__device__ __forceinline__ void exp2_poly(float x0, float x1, float& y0, float& y1) {
-  float c0, c1;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(c0) : "f"(x0), "f"(-127.0f));
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(c1) : "f"(x1), "f"(-127.0f));
-  const uint64_t x = pack2(c0, c1);
-  const uint64_t big = pack2(12582912.0f, 12582912.0f), nbig = pack2(-12582912.0f, -12582912.0f), neg = pack2(-1.0f, -1.0f);
-  const uint64_t t = add2(x, big);                   // n in the low bits of the mantissa
-  const uint64_t f = fma2(add2(t, nbig), neg, x);
-  uint64_t p = fma2(f, pack2(1.3276476e-3f, 1.3276476e-3f), pack2(9.675541e-3f, 9.675541e-3f));
-  p = fma2(p, f, pack2(5.550713e-2f, 5.550713e-2f));
-  p = fma2(p, f, pack2(0.2402212f, 0.2402212f));
-  p = fma2(p, f, pack2(0.69314694f, 0.69314694f));
-  p = fma2(p, f, pack2(1.0000001f, 1.0000001f));
-  float t0, t1, p0, p1;
-  unpack2(t, t0, t1);
-  unpack2(p, p0, p1);
-  y0 = __uint_as_float(__float_as_uint(p0) + (__float_as_uint(t0) << 23));
-  y1 = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(t1) << 23));
-}
-constexpr int POLY_OF_8 = 2;      // of eight pairs of exponentials, how many go to the FMA pipe
-
-// Two CTAs an SM, each with 128 query rows: while one turns scores into probabilities the other's products run.  K and V tiles take
-// turns in the ring; a score tile takes 128 columns of TMEM and O another 64 DC.
-template <int DC> constexpr int FWD_STAGES = DC == 1 ? 4 : 2;
+// Two CTAs an SM, each with 128 query rows, against tiles of 64 keys: two of them in TMEM (64 columns each, beside O's 64 DC), so that a
+// tile's scores are there when the warps come from the one before, and the products of two CTAs fill the tensor pipe.  (8 x 2048 tokens,
+// 32/8 heads of 128, causal: 273 us; key tiles of 128, one at a time, 292: 1506 of a tile's 3644 cycles went by between the last P and the
+// next scores.)  What bounds it: 64-wide products with A in shared memory take 427 cycles for 256 of arithmetic, so that the tensor pipe is
+// busy 78 % of the time; the exponentials take 58 % of theirs.  (A part of them as polynomials on the FMA pipe: 298 us for one in eight of
+// the pairs, 303 for two; the warps' issue slots were what it cost.)
+constexpr int FWD_TN = 64;
+template <int DC> constexpr int FWD_STAGES = DC == 1 ? 8 : 5;
 constexpr int FWD_THREADS = 192;
 
 template <int DC>
 __global__ void __launch_bounds__(FWD_THREADS, 2)
 attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                 const __grid_constant__ UmmaCall P) {
-  constexpr int STAGES = FWD_STAGES<DC>, TILE = DC * CHUNK<128>;
+  constexpr int STAGES = FWD_STAGES<DC>, TN = FWD_TN, OWN = DC * CHUNK<128>, TILE = DC * CHUNK<TN>;
   extern __shared__ __align__(1024) uint8_t smem[];
-  uint8_t *sq = smem, *ring = smem + TILE;
+  uint8_t *sq = smem, *ring = smem + OWN;
   Shared& s = *reinterpret_cast<Shared*>(ring + STAGES * TILE);
   const AttnCall& C = P.c;
   if (!in_place(smem, C.seqs.status)) return;
   begin(s, P, STAGES, 4, 0, 256);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t ts = s.tmem, to = s.tmem + 128;
+  const uint32_t ts = s.tmem, to = s.tmem + 2 * TN;
   volatile int* ab = &s.abort_flag;
   int32_t* status = C.seqs.status;
-  auto tiles_of = [&](const Item& it) { return ((C.causal ? min(it.len, it.t0 + 128) : it.len) + 127) / 128; };
+  auto tiles_of = [&](const Item& it) { return ((C.causal ? min(it.len, it.t0 + 128) : it.len) + TN - 1) / TN; };
 
   if (warp == 5) {
     Ring r;
@@ -347,14 +331,17 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
       bool ok = warp_wait(&s.own_empty, (n & 1) ^ 1, ab, status);
       if (!ok) break;
       if (elect_one()) {
-        mbar_expect_tx(&s.own_full, TILE);
+        mbar_expect_tx(&s.own_full, OWN);
         load_tile<DC, 128>(sq, &mq, it.head, it.first + it.t0, &s.own_full);
       }
       ++own;
       const int tiles = tiles_of(it), kv = it.head / C.group;
       const bool stall = P.stall_once && blockIdx.x == 0 && n == 0;
-      for (int i = 0; i < 2 * tiles && ok; ++i)
-        ok = fill<DC, 128>(s, r, STAGES, ring, (i & 1) ? &mv : &mk, kv, it.first + (i >> 1) * 128, stall && i == 0, status);
+      // in the order of their use: K 0, K 1, V 0, K 2, V 1, ...
+      for (int j = 0; j <= tiles && ok; ++j) {
+        if (j < tiles) ok = fill<DC, TN>(s, r, STAGES, ring, &mk, kv, it.first + j * TN, stall && j == 0, status);
+        if (j > 0) ok = ok && fill<DC, TN>(s, r, STAGES, ring, &mv, kv, it.first + (j - 1) * TN, false, status);
+      }
       if (!ok) break;
     }
     if (lane == 0) drain(s, r, STAGES, own, status);
@@ -362,131 +349,141 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     const bool leader = elect_one();
     Ring r;
     Item it;
-    uint32_t made = 0;                   // P tiles so far
+    uint32_t made = 0, score = 0;        // P tiles, score tiles so far
     bool ok = true;
     for (int n = 0; ok && get_item(s, n, status, it); ++n) {
       const int tiles = tiles_of(it);
       ok = warp_wait(&s.own_full, n & 1, ab, status);
+      if (!ok) break;
+      auto scores = [&](bool last) {
+        ok = warp_wait(&s.full[r.stage], r.phase, ab, status);
+        if (!ok) return;
+        tc_fence_after();
+        if (leader) {
+          product_tiles<DC, TN>(ts + (score & 1) * TN, smem_u32(sq), smem_u32(ring + r.stage * TILE));
+          umma_commit(&s.empty[r.stage]);
+          umma_commit(&s.scores[score & 1]);
+          if (last) umma_commit(&s.own_empty);
+        }
+        ++score;
+        r.next(STAGES);
+      };
+      scores(tiles == 1);
+      if (ok && tiles > 1) scores(tiles == 2);
       for (int j = 0; j < tiles && ok; ++j, ++made) {
         ok = warp_wait(&s.full[r.stage], r.phase, ab, status);
         if (!ok) break;
-        tc_fence_after();
-        if (leader) {
-          product_tiles<DC, 128>(ts, smem_u32(sq), smem_u32(ring + r.stage * TILE));
-          umma_commit(&s.empty[r.stage]);
-          umma_commit(&s.scores[0]);
-          if (j == tiles - 1) umma_commit(&s.own_empty);
-        }
-        r.next(STAGES);
-        ok = warp_wait(&s.full[r.stage], r.phase, ab, status);
-        if (!ok) break;
-        uint8_t* v = ring + r.stage * TILE;
-        const int have = it.len - j * 128;
-        if (have < 128) {
-          zero_rows<DC, 128>(v, have, lane);
+        const int have = it.len - j * TN, place = r.stage;
+        if (have < TN) {
+          zero_rows<DC, TN>(ring + place * TILE, have, lane);
           fence_async_smem();
           __syncwarp();
         }
+        r.next(STAGES);
         if (j == 0) ok = warp_wait(&s.acc_empty, (n & 1) ^ 1, ab, status);
-        // the lower half of P's columns, then the upper, as they come
-        ok = ok && warp_wait(&s.ready[0], made & 1, ab, status);
-        if (!ok) break;
-        tc_fence_after();
-        if (leader) product_rows<DC, 128, 0, 4>(to, ts, 32, smem_u32(v), j != 0);
-        ok = warp_wait(&s.ready[1], made & 1, ab, status);
+        ok = ok && warp_wait(&s.ready[made & 1], (made >> 1) & 1, ab, status);
         if (!ok) break;
         tc_fence_after();
         if (leader) {
-          product_rows<DC, 128, 4, 8>(to, ts, 32, smem_u32(v), true);
-          umma_commit(&s.empty[r.stage]);
+          product_rows<DC, TN, 0, TN / 16>(to, ts + (made & 1) * TN, 0, smem_u32(ring + place * TILE), j != 0);
+          umma_commit(&s.empty[place]);
+          umma_commit(&s.added);
           if (j == tiles - 1) umma_commit(&s.done);
         }
-        r.next(STAGES);
+        if (j + 2 < tiles) scores(j + 3 == tiles);
       }
     }
     if (leader && *ab) drain_products(&s.drain, ab, status);
   } else {
     const uint32_t lanes = (uint32_t)(warp * 32) << 16;
     const float c = C.scale * ATTN_LOG2E, none = __int_as_float(0xff800000);
+    const uint64_t c2 = pack2(c, c);
     Item it;
     uint32_t made = 0;
     bool ok = true;
     for (int n = 0; ok && get_item(s, n, status, it); ++n) {
       const int row = it.t0 + threadIdx.x, tiles = tiles_of(it);         // row: in the sequence
-      float m = none, l = 0.f;
+      // Sums are relative to 2^m, m near the largest score so far (times c).  They are floats, so it need not be the largest:
+      // exponentials are taken before the tile's own maximum is known (with it first, 395 cycles per 128 keys went by without an
+      // exponential on its way), m follows once the maximum is 8 above it, and at once where 2^64 is passed.
+      float m = 0.f, l = 0.f, over = 0.f;            // over: the last tile's maximum above m
+      auto lift = [&](float by, bool mine) {
+        // O must be complete up to the tile before this one
+        ok = warp_wait(&s.added, (made - 1) & 1, ab, status);
+        if (!ok) return;
+        tc_fence_after();
+        const float f = mine ? attn_exp2(-by) : 1.0f;
+        m += mine ? by : 0.f;
+        l *= f;
+#pragma unroll
+        for (int q = 0; q < 2 * DC; ++q) {
+          uint32_t o[32];
+          tmem_ld32(to + lanes + q * 32, o);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+          tmem_st32(to + lanes + q * 32, o);
+        }
+        tmem_wait_st();
+      };
       for (int j = 0; j < tiles; ++j, ++made) {
-        ok = warp_wait(&s.scores[0], made & 1, ab, status);
+        ok = warp_wait(&s.scores[made & 1], (made >> 1) & 1, ab, status);
         if (!ok) break;
         tc_fence_after();
-        uint32_t a[64], b[64];
-        tmem_ld64(ts + lanes, a);
-        tmem_ld64(ts + lanes + 64, b);
+        const uint32_t at = ts + lanes + (made & 1) * TN;
         // columns this row sees in the tile
-        const int see = min(128, (C.causal ? min(it.len, row + 1) : it.len) - j * 128);
-        const bool cut = __any_sync(0xffffffffu, see < 128);
-        if (cut) {
+        const int see = min(TN, (C.causal ? min(it.len, row + 1) : it.len) - j * TN);
+        const bool cut = __any_sync(0xffffffffu, see < TN);
+        uint32_t x[64], o[32];
+        auto read = [&]() {
+          tmem_ld64(at, x);
+          if (cut) {
 #pragma unroll
-          for (int i = 0; i < 64; ++i) {
-            a[i] = i < see ? a[i] : 0xff800000u;
-            b[i] = i + 64 < see ? b[i] : 0xff800000u;
+            for (int i = 0; i < 64; ++i) x[i] = i < see ? x[i] : 0xff800000u;
           }
-        }
-        float t[4] = {none, none, none, none};
-#pragma unroll
-        for (int i = 0; i < 64; ++i) t[i & 3] = fmaxf(t[i & 3], fmaxf(__uint_as_float(a[i]), __uint_as_float(b[i])));
-        const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+        };
+        read();
         if (j == 0) {
-          m = top;
-        } else {
-          // the sums are relative to m; it follows the maximum once that has risen far enough for P to lose range
-          const bool rise = (top - m) * c > 8.0f;
-          if (__any_sync(0xffffffffu, rise)) {
-            const float f = rise ? attn_exp2((m - top) * c) : 1.0f;
-            m = rise ? top : m;
-            l *= f;
+          float t[4] = {none, none, none, none};
 #pragma unroll
-            for (int q = 0; q < 2 * DC; ++q) {
-              uint32_t o[32];
-              tmem_ld32(to + lanes + q * 32, o);
-#pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-              tmem_st32(to + lanes + q * 32, o);
-            }
-          }
+          for (int i = 0; i < 64; ++i) t[i & 3] = fmaxf(t[i & 3], __uint_as_float(x[i]));
+          m = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) * c;
+          if (m == none) m = 0.f;
+        } else if (__any_sync(0xffffffffu, over > 8.0f)) {
+          lift(over, over > 8.0f);
+          if (!ok) break;
         }
-        const float ref = m == none ? 0.f : m;
-        const uint64_t c2 = pack2(c, c), n2 = pack2(-ref * c, -ref * c);
-        uint64_t l2[2] = {0, 0};
-        auto half = [&](const uint32_t (&x)[64], uint32_t at, uint64_t* bar, bool poly) {
-          uint32_t o[32];
+        float sum;
+        auto exps = [&]() {
+          const uint64_t n2 = pack2(-m, -m);
+          uint64_t l2[2] = {0, 0};
+          float t[2] = {none, none};
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
             float e0, e1;
             unpack2(fma2(pack2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), c2, n2), e0, e1);
-            if (poly && (i * POLY_OF_8) % 8 < POLY_OF_8) {
-              exp2_poly(e0, e1, e0, e1);
-            } else {
-              e0 = attn_exp2(e0);
-              e1 = attn_exp2(e1);
-            }
+            t[i & 1] = fmaxf(t[i & 1], fmaxf(e0, e1));
+            e0 = attn_exp2(e0);
+            e1 = attn_exp2(e1);
             l2[i & 1] = add2(l2[i & 1], pack2(e0, e1));
             o[i] = pack_bf16(e0, e1);
           }
-          tmem_st32(at, o);
-          tmem_wait_st();
-          tc_fence_before();
-          warp_arrive(bar);
+          float y0, y1;
+          unpack2(add2(l2[0], l2[1]), y0, y1);
+          sum = y0 + y1;
+          over = fmaxf(t[0], t[1]);
         };
-        if (cut) {                       // masked places have to become 0 exactly
-          half(a, ts + lanes, &s.ready[0], false);
-          half(b, ts + lanes + 32, &s.ready[1], false);
-        } else {
-          half(a, ts + lanes, &s.ready[0], true);
-          half(b, ts + lanes + 32, &s.ready[1], true);
+        exps();
+        if (j != 0 && __any_sync(0xffffffffu, over > 64.0f)) {
+          lift(over, over > 64.0f);
+          if (!ok) break;
+          read();
+          exps();
         }
-        float x0, x1;
-        unpack2(add2(l2[0], l2[1]), x0, x1);
-        l += x0 + x1;
+        l += sum;
+        tmem_st32(at, o);
+        tmem_wait_st();
+        tc_fence_before();
+        warp_arrive(&s.ready[made & 1]);
       }
       ok = ok && warp_wait(&s.done, n & 1, ab, status);
       if (!ok) break;
@@ -494,7 +491,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
       store_rows<DC>(to + lanes, C.o, (int64_t)it.first + it.t0 + warp * 32, it.head, C.dim, it.len - it.t0 - warp * 32, 1.0f / l);
       tc_fence_before();
       warp_arrive(&s.acc_empty);
-      if (row < it.len) C.lse[(int64_t)it.head * C.seqs.total + it.first + row] = (m * c) * ATTN_LN2 + logf(l);
+      if (row < it.len) C.lse[(int64_t)it.head * C.seqs.total + it.first + row] = m * ATTN_LN2 + logf(l);
     }
   }
   end(s, P, 256);
@@ -985,12 +982,12 @@ bool attn_umma_ok(const Attn* a, const AttnCall& c, bool backward) {
 cudaError_t launch_attn_umma_fwd(const Attn* a, const AttnCall& c, cudaStream_t st) {
   const int total = c.seqs.total;
   CUtensorMap mq, mk, mv;
-  if (!attn_map(&mq, c.q, c.heads_q, c.dim, total, 128) || !attn_map(&mk, c.k, c.heads_kv, c.dim, total, 128) ||
-      !attn_map(&mv, c.v, c.heads_kv, c.dim, total, 128))
+  if (!attn_map(&mq, c.q, c.heads_q, c.dim, total, 128) || !attn_map(&mk, c.k, c.heads_kv, c.dim, total, FWD_TN) ||
+      !attn_map(&mv, c.v, c.heads_kv, c.dim, total, FWD_TN))
     return cudaErrorInvalidValue;
   const long tiles = tile_bound(total, c.seqs.N, 128) * c.heads_q;
-  return c.dim <= 64 ? run(attn_fwd_kernel<1>, false, 0, (1 + FWD_STAGES<1>) * CHUNK<128>, FWD_THREADS, 2, tiles, a, c, st, mq, mk, mv)
-                     : run(attn_fwd_kernel<2>, false, 0, (1 + FWD_STAGES<2>) * 2 * CHUNK<128>, FWD_THREADS, 2, tiles, a, c, st, mq, mk, mv);
+  return c.dim <= 64 ? run(attn_fwd_kernel<1>, false, 0, CHUNK<128> + FWD_STAGES<1> * CHUNK<FWD_TN>, FWD_THREADS, 2, tiles, a, c, st, mq, mk, mv)
+                     : run(attn_fwd_kernel<2>, false, 0, 2 * (CHUNK<128> + FWD_STAGES<2> * CHUNK<FWD_TN>), FWD_THREADS, 2, tiles, a, c, st, mq, mk, mv);
 }
 
 cudaError_t launch_attn_umma_bwd(const Attn* a, const AttnCall& c, cudaStream_t st) {
