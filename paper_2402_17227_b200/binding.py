@@ -412,8 +412,9 @@ def _need(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
-def _stream_of(device: torch.device):
-    return _raw_stream(device.index) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
+def _stream_at(index: int):
+    """The current stream of a device."""
+    return _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream(index).cuda_stream
 
 
 def _on(device, what: str, *tensors) -> None:
@@ -434,6 +435,7 @@ class _Handle:
 
     def _create(self, desc) -> None:
         self.device = _current_device()
+        self._index = self.device.index
         self._h = C.c_void_p(None)
         _check(getattr(lib(), f"vcas_{self._kind}_create")(C.byref(self._h), C.byref(desc)), f"vcas_{self._kind}_create")
 
@@ -464,65 +466,70 @@ class Attention(_Handle):
         _need(dtype in _DTYPES, "attention is in bfloat16 or float32")
         self.heads_q, self.heads_kv, self.head_dim, self.dtype = heads_q, heads_kv, head_dim, dtype
         self._create(AttnDesc(max_tokens, max_seqs, heads_q, heads_kv, head_dim, _DTYPES[dtype], 1 if causal else 0, scale))
+        # the tensors of a call as the library takes them: filled anew by every call (d_o, q, k, v, o, dq, dk, dv)
+        self._args = [AttnTensor() for _ in range(8)]
+        self._refs = [C.byref(a) for a in self._args]
 
-    def _tensor(self, t, total: int, heads: int, written: bool = False) -> AttnTensor:
-        _need(t.shape == (total, heads, self.head_dim) and t.dtype == self.dtype,
-              f"expected [{total}, {heads}, {self.head_dim}] of {self.dtype}, got {tuple(t.shape)} of {t.dtype}")
-        _need(t.device == self.device, f"tensors of a call on {self.device} only")
+    def _tensor(self, place: int, t, total: int, heads: int, written: bool = False):
+        if t.shape != (total, heads, self.head_dim) or t.dtype is not self.dtype:
+            raise ValueError(f"expected [{total}, {heads}, {self.head_dim}] of {self.dtype}, got {tuple(t.shape)} of {t.dtype}")
+        if t.get_device() != self._index:
+            raise ValueError(f"tensors of a call on {self.device} only")
         token, head, inner = t.stride()
-        _need(inner == 1 or self.head_dim == 1, "a head's values lie side by side")
+        if inner != 1 and self.head_dim != 1:
+            raise ValueError("a head's values lie side by side")
         if written:      # no two elements in one place
-            a, b = sorted(((token, total), (head, heads)))
             least = self.head_dim
-            for stride, n in (a, b):
-                _need(n <= 1 or stride >= least, "rows of an output overlap")
-                least = max(least, stride * n) if n > 1 else least
-        return AttnTensor(t.data_ptr(), token, head)
+            for stride, n in ((token, total), (head, heads)) if token < head else ((head, heads), (token, total)):
+                if n > 1:
+                    if stride < least:
+                        raise ValueError("rows of an output overlap")
+                    least = stride * n
+        a = self._args[place]
+        a.ptr, a.token, a.head = t.data_ptr(), token, head
+        return self._refs[place]
 
-    def _sequences(self, q, starts):
-        _need(starts.dim() == 1 and starts.numel() >= 1 and starts.dtype == torch.int32 and starts.is_contiguous(),
-              "starts is int32 [N + 1]")
-        _on(self.device, "starts", starts)
-        return q.shape[0], starts.numel() - 1
+    def _sequences(self, starts):
+        if starts.dim() != 1 or starts.dtype is not torch.int32 or not starts.is_contiguous() or starts.get_device() != self._index:
+            raise ValueError(f"starts is int32 [N + 1] on {self.device}")
+        n = starts.shape[0] - 1
+        _need(n >= 0, "starts is int32 [N + 1]")
+        return n
 
     def _lse(self, lse, total):
-        _need(lse.shape == (self.heads_q, total) and lse.dtype == torch.float32 and lse.is_contiguous(),
-              "lse is float32 [heads_q, total]")
-        _on(self.device, "lse", lse)
+        if lse.shape != (self.heads_q, total) or lse.dtype is not torch.float32 or not lse.is_contiguous() or \
+                lse.get_device() != self._index:
+            raise ValueError(f"lse is float32 [heads_q, total] on {self.device}")
         return lse.data_ptr()
 
     def fwd(self, q, k, v, starts, *, o=None, lse=None):
         """Returns (o, lse)."""
-        total, N = self._sequences(q, starts)
+        total, N, Hq, Hk, T = q.shape[0], self._sequences(starts), self.heads_q, self.heads_kv, self._tensor
         if o is None:
-            o = torch.empty(total, self.heads_q, self.head_dim, dtype=self.dtype, device=self.device)
+            o = torch.empty(total, Hq, self.head_dim, dtype=self.dtype, device=self.device)
         if lse is None:
-            lse = torch.empty(self.heads_q, total, dtype=torch.float32, device=self.device)
-        r, Hq, Hk = C.byref, self.heads_q, self.heads_kv
-        _check(lib().vcas_attn_fwd(self._h, r(self._tensor(q, total, Hq)), r(self._tensor(k, total, Hk)),
-                                   r(self._tensor(v, total, Hk)), starts.data_ptr(), N, total,
-                                   r(self._tensor(o, total, Hq, True)), self._lse(lse, total), _stream_of(self.device)),
-               "vcas_attn_fwd")
+            lse = torch.empty(Hq, total, dtype=torch.float32, device=self.device)
+        _check(lib().vcas_attn_fwd(self._h, T(1, q, total, Hq), T(2, k, total, Hk), T(3, v, total, Hk), starts.data_ptr(), N, total,
+                                   T(4, o, total, Hq, True), self._lse(lse, total), _stream_at(self._index)), "vcas_attn_fwd")
         return o, lse
 
     def bwd(self, d_o, q, k, v, o, lse, starts, *, dq=None, dk=None, dv=None, alive_in=None, alive_cnt_in=None,
             skip_dropped_rows: bool = False):
         """Returns (dq, dk, dv).  alive_in, alive_cnt_in: the kept_out, kept_cnt_out of the layer above."""
-        total, N = self._sequences(q, starts)
-        Hq, Hk, D = self.heads_q, self.heads_kv, self.head_dim
-        new = lambda h: torch.empty(total, h, D, dtype=self.dtype, device=self.device)
+        total, N, Hq, Hk, T = q.shape[0], self._sequences(starts), self.heads_q, self.heads_kv, self._tensor
+        new = lambda h: torch.empty(total, h, self.head_dim, dtype=self.dtype, device=self.device)
         dq, dk, dv = new(Hq) if dq is None else dq, new(Hk) if dk is None else dk, new(Hk) if dv is None else dv
-        _need((alive_in is None) == (alive_cnt_in is None), "alive_in and alive_cnt_in come together")
-        if alive_in is not None:
-            _need(alive_in.dtype == alive_cnt_in.dtype == torch.int32 and alive_in.numel() >= N and alive_cnt_in.numel() >= 1
-                  and alive_in.is_contiguous(), "alive_in is int32 [N], alive_cnt_in int32 [1]")
+        alive = cnt = None
+        if alive_in is not None or alive_cnt_in is not None:
+            if alive_in is None or alive_cnt_in is None or alive_in.dtype is not torch.int32 or alive_cnt_in.dtype is not torch.int32 \
+                    or alive_in.numel() < N or alive_cnt_in.numel() < 1 or not alive_in.is_contiguous():
+                raise ValueError("alive_in is int32 [N], alive_cnt_in int32 [1], and they come together")
             _on(self.device, "alive_in", alive_in, alive_cnt_in)
-        r, dp = C.byref, lambda t: None if t is None else t.data_ptr()
-        T = self._tensor
-        _check(lib().vcas_attn_bwd(self._h, r(T(d_o, total, Hq)), r(T(q, total, Hq)), r(T(k, total, Hk)), r(T(v, total, Hk)),
-                                   r(T(o, total, Hq)), self._lse(lse, total), starts.data_ptr(), N, total, dp(alive_in),
-                                   dp(alive_cnt_in), 1 if skip_dropped_rows else 0, r(T(dq, total, Hq, True)),
-                                   r(T(dk, total, Hk, True)), r(T(dv, total, Hk, True)), _stream_of(self.device)), "vcas_attn_bwd")
+            alive, cnt = alive_in.data_ptr(), alive_cnt_in.data_ptr()
+        _check(lib().vcas_attn_bwd(self._h, T(0, d_o, total, Hq), T(1, q, total, Hq), T(2, k, total, Hk), T(3, v, total, Hk),
+                                   T(4, o, total, Hq), self._lse(lse, total), starts.data_ptr(), N, total, alive, cnt,
+                                   1 if skip_dropped_rows else 0, T(5, dq, total, Hq, True), T(6, dk, total, Hk, True),
+                                   T(7, dv, total, Hk, True), _stream_at(self._index)), "vcas_attn_bwd")
         return dq, dk, dv
 
     def set_wait_limit(self, limit_ns: int, stall_once: bool = False) -> None:
@@ -554,44 +561,55 @@ class TokenLoss(_Handle):
         self._create(LossDesc(max_rows, vocab, _DTYPES[dtype], top))
 
     def _rows(self, logits, tokens):
-        _need(logits.dim() == 2 and logits.shape[1] == self.vocab and logits.dtype == self.dtype,
-              f"logits are [rows, {self.vocab}] of {self.dtype}")
-        _need(logits.stride(1) == 1 or self.vocab == 1, "a row's logits lie side by side")
+        """Rows and the elements between them."""
+        V = self.vocab
+        if logits.dim() != 2 or logits.shape[1] != V or logits.dtype is not self.dtype or logits.get_device() != self._index:
+            raise ValueError(f"logits are [rows, {V}] of {self.dtype} on {self.device}")
         rows = logits.shape[0]
-        _need(rows <= 1 or logits.stride(0) >= self.vocab, "rows that overlap")
-        _need(tokens.shape == (rows,) and tokens.is_contiguous() and tokens.dtype in (torch.int32, torch.int64),
-              "tokens are [rows], int32 or int64")
-        _on(self.device, "logits and tokens", logits, tokens)
-        return rows, max(logits.stride(0), self.vocab)
+        ld, inner = logits.stride()
+        if inner != 1 and V != 1:
+            raise ValueError("a row's logits lie side by side")
+        if ld < V:
+            if rows > 1:
+                raise ValueError("rows that overlap")
+            ld = V
+        if tokens.shape != (rows,) or tokens.dtype not in (torch.int64, torch.int32) or not tokens.is_contiguous() or \
+                tokens.get_device() != self._index:
+            raise ValueError(f"tokens are [rows], int32 or int64, on {self.device}")
+        return rows, ld
 
     def fwd(self, logits, tokens) -> LogProbs:
         """tokens: [rows], negative where there is none."""
         rows, ld = self._rows(logits, tokens)
-        f = torch.empty(3, rows, dtype=torch.float32, device=self.device)
-        tl = torch.empty(rows, self.top, dtype=torch.float32, device=self.device) if self.top else None
-        ti = torch.empty(rows, self.top, dtype=torch.int32, device=self.device) if self.top else None
-        base = f.data_ptr()
-        _check(lib().vcas_loss_fwd(self._h, logits.data_ptr(), ld, tokens.data_ptr(), tokens.element_size(), rows, base,
-                                   base + 4 * rows, base + 8 * rows, None if tl is None else tl.data_ptr(),
-                                   None if ti is None else ti.data_ptr(), _stream_of(self.device)), "vcas_loss_fwd")
-        return LogProbs(f[0], f[1], f[2], tl, ti)
+        lse, logp, entropy = torch.empty((3, rows), dtype=torch.float32, device=self.device).unbind(0)
+        tl = ti = None
+        if self.top:
+            tl = torch.empty((rows, self.top), dtype=torch.float32, device=self.device)
+            ti = torch.empty((rows, self.top), dtype=torch.int32, device=self.device)
+        base = lse.data_ptr()
+        _check(lib().vcas_loss_fwd(self._h, logits.data_ptr(), ld, tokens.data_ptr(), tokens.element_size(), rows, base + 4 * rows,
+                                   base + 8 * rows, base, tl.data_ptr() if self.top else None, ti.data_ptr() if self.top else None,
+                                   _stream_at(self._index)), "vcas_loss_fwd")
+        return LogProbs(logp, entropy, lse, tl, ti)
 
     def bwd(self, logits, tokens, lse, g_logp, *, entropy=None, g_entropy=None, dlogits=None, a_out=None):
         """Returns (dlogits, a_out); dlogits may be logits itself.  a_out: the rows' square-norms for linear_bwd_chain(a_in=)."""
         rows, ld = self._rows(logits, tokens)
-        vectors = [lse, g_logp] + [t for t in (entropy, g_entropy, a_out) if t is not None]
-        _need(all(t.shape == (rows,) and t.dtype == torch.float32 and t.is_contiguous() for t in vectors),
-              "lse, entropy and the derivatives are [rows] of float32")
         if dlogits is None:
-            dlogits = torch.empty(rows, self.vocab, dtype=self.dtype, device=self.device)
+            dlogits = torch.empty((rows, self.vocab), dtype=self.dtype, device=self.device)
         if a_out is None:
             a_out = torch.empty(rows, dtype=torch.float32, device=self.device)
-        _, ld_d = self._rows(dlogits, tokens)
-        _on(self.device, "lse, entropy and the derivatives", a_out, *vectors)
-        dp = lambda t: None if t is None else t.data_ptr()
-        _check(lib().vcas_loss_bwd(self._h, logits.data_ptr(), ld, tokens.data_ptr(), tokens.element_size(), rows, dp(lse),
-                                   dp(entropy), dp(g_logp), dp(g_entropy), dp(dlogits), ld_d, dp(a_out),
-                                   _stream_of(self.device)), "vcas_loss_bwd")
+        ld_d = ld if dlogits is logits else self._rows(dlogits, tokens)[1]
+        at = []
+        for t in (lse, entropy, g_logp, g_entropy, a_out):
+            if t is None:
+                at.append(None)
+                continue
+            if t.shape != (rows,) or t.dtype is not torch.float32 or not t.is_contiguous() or t.get_device() != self._index:
+                raise ValueError(f"lse, entropy, the derivatives and a_out are [rows] of float32 on {self.device}")
+            at.append(t.data_ptr())
+        _check(lib().vcas_loss_bwd(self._h, logits.data_ptr(), ld, tokens.data_ptr(), tokens.element_size(), rows, at[0], at[1], at[2],
+                                   at[3], dlogits.data_ptr(), ld_d, at[4], _stream_at(self._index)), "vcas_loss_bwd")
         return dlogits, a_out
 
 
@@ -664,14 +682,19 @@ class AdamW:
         """step: 1 for the first.  seed: another one each step (8-bit states).  grad_scale: float32 [1] on the device.
         rates (adamw_rates, float32 [3]) and seed_dev (int64 [1]) on the device are read in place of lr and step, and of seed:
         a captured step then follows them."""
-        ok = lambda t, n, dt: t is None or (t.dtype == dt and t.numel() == n and t.is_contiguous())
-        _need(ok(grad_scale, 1, torch.float32) and ok(rates, 3, torch.float32) and ok(seed_dev, 1, torch.int64),
-              "grad_scale is float32 [1], rates float32 [3], seed_dev int64 [1]")
-        _on(self.device, "grad_scale, rates and seed_dev", grad_scale, rates, seed_dev)
-        dp = lambda t: None if t is None else t.data_ptr()
-        args = AdamWArgs(lr, beta1, beta2, eps, step, seed & 0xFFFFFFFFFFFFFFFF, dp(grad_scale), dp(rates), dp(seed_dev))
-        with torch.cuda.device(self.device):
-            _check(lib().vcas_adamw_step(self._table, len(self.tensors), C.byref(args), _stream_of(self.device)), "vcas_adamw_step")
+        at = []
+        for t, n, dt in ((grad_scale, 1, torch.float32), (rates, 3, torch.float32), (seed_dev, 1, torch.int64)):
+            if t is not None and (t.dtype is not dt or t.numel() != n or not t.is_contiguous() or t.device != self.device):
+                raise ValueError(f"grad_scale is float32 [1], rates float32 [3], seed_dev int64 [1], on {self.device}")
+            at.append(None if t is None else t.data_ptr())
+        args = AdamWArgs(lr, beta1, beta2, eps, step, seed & 0xFFFFFFFFFFFFFFFF, *at)
+        call = lambda: lib().vcas_adamw_step(self._table, len(self.tensors), C.byref(args), _stream_at(self.device.index))
+        if torch.cuda.current_device() == self.device.index:
+            rc = call()
+        else:
+            with torch.cuda.device(self.device):
+                rc = call()
+        _check(rc, "vcas_adamw_step")
 
 
 def adamw_rates(lr: float, beta1: float, beta2: float, step: int) -> torch.Tensor:

@@ -20,15 +20,48 @@ __device__ __forceinline__ float widen(__nv_bfloat16 x) { return __bfloat162floa
 __device__ __forceinline__ void put(float* p, float x) { *p = x; }
 __device__ __forceinline__ void put(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 
-// rows t0 .. t0 + 63 of one head into shared memory, zeros behind the sequence's end and the head's width
+// Rows t0 .. t0 + 63 of one head, zeros behind the sequence's end and the head's width: a thread's share in registers (all of its loads
+// are on their way at once), then in shared memory.  fp32 rows that allow it are read 16 bytes at a time.
+template <typename T, int DP>
+struct TileLoad {
+  static constexpr int N = TILE * DP / 4 / THREADS;
+  float4 v[N];
+  __device__ __forceinline__ void get(const Strided& x, int first, int len, int t0, int head, int dim) {
+    const T* base = (const T*)x.p + (int64_t)head * x.head + (int64_t)(first + t0) * x.token;
+    const bool wide = sizeof(T) == 4 && ((uintptr_t)base & 15) == 0 && (x.token & 3) == 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int at = (threadIdx.x + i * THREADS) * 4, r = at / DP, d = at % DP;
+      v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (t0 + r < len && d < dim) {       // dim is a multiple of 8
+        const T* p = base + (int64_t)r * x.token + d;
+        if (wide) v[i] = __ldg(reinterpret_cast<const float4*>(p));
+        else v[i] = make_float4(widen(p[0]), widen(p[1]), widen(p[2]), widen(p[3]));
+      }
+    }
+  }
+  __device__ __forceinline__ void put(float* dst) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int at = (threadIdx.x + i * THREADS) * 4;
+      *reinterpret_cast<float4*>(dst + at / DP * (DP + 4) + at % DP) = v[i];
+    }
+  }
+};
 template <typename T, int DP>
 __device__ __forceinline__ void load_tile(float* dst, const Strided& x, int first, int len, int t0, int head, int dim) {
-  const T* base = (const T*)x.p + (int64_t)head * x.head;
-#pragma unroll 4
-  for (int i = threadIdx.x; i < TILE * DP; i += THREADS) {
-    const int r = i / DP, d = i % DP;
-    dst[r * (DP + 4) + d] = t0 + r < len && d < dim ? widen(base[(int64_t)(first + t0 + r) * x.token + d]) : 0.f;
-  }
+  TileLoad<T, DP> l;
+  l.get(x, first, len, t0, head, dim);
+  l.put(dst);
+}
+template <typename T, int DP>
+__device__ __forceinline__ void load_two(float* da, const Strided& a, float* db, const Strided& b, int first, int len, int t0, int head,
+                                         int dim) {
+  TileLoad<T, DP> la, lb;
+  la.get(a, first, len, t0, head, dim);
+  lb.get(b, first, len, t0, head, dim);
+  la.put(da);
+  lb.put(db);
 }
 // s[i][j] = sum_d a[ty * 4 + i][d] b[tx + 16 j][d]
 template <int DP>
@@ -122,8 +155,7 @@ __global__ void __launch_bounds__(THREADS) attn_fma_fwd_kernel(AttnCall C) {
   }
   for (int j0 = 0; j0 < end; j0 += TILE) {
     __syncthreads();
-    load_tile<T, DP>(sk, C.k, p.first, p.len, j0, p.head / C.group, C.dim);
-    load_tile<T, DP>(sv, C.v, p.first, p.len, j0, p.head / C.group, C.dim);
+    load_two<T, DP>(sk, C.k, sv, C.v, p.first, p.len, j0, p.head / C.group, C.dim);
     __syncthreads();
     float s[4][4];
     dots<DP>(sq, sk, tx, ty, s);
@@ -203,8 +235,7 @@ __global__ void __launch_bounds__(THREADS) attn_fma_dq_kernel(AttnCall C) {
   const Place p = place_of(C.seqs, C.heads_q, C.causal);
   if (!p.any) return;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  load_tile<T, DP>(sq, C.q, p.first, p.len, p.t0, p.head, C.dim);
-  load_tile<T, DP>(sdo, C.d_o, p.first, p.len, p.t0, p.head, C.dim);
+  load_two<T, DP>(sq, C.q, sdo, C.d_o, p.first, p.len, p.t0, p.head, C.dim);
   float lse[4], delta[4], acc[4][DP / 16];
   row_values(C, p, p.t0, p.head, ty, lse, delta);
 #pragma unroll
@@ -214,8 +245,7 @@ __global__ void __launch_bounds__(THREADS) attn_fma_dq_kernel(AttnCall C) {
   const int end = C.causal ? min(p.len, p.t0 + TILE) : p.len;
   for (int j0 = 0; j0 < end; j0 += TILE) {
     __syncthreads();
-    load_tile<T, DP>(sk, C.k, p.first, p.len, j0, p.head / C.group, C.dim);
-    load_tile<T, DP>(sv, C.v, p.first, p.len, j0, p.head / C.group, C.dim);
+    load_two<T, DP>(sk, C.k, sv, C.v, p.first, p.len, j0, p.head / C.group, C.dim);
     __syncthreads();
     float s[4][4], dp[4][4];
     dots<DP>(sq, sk, tx, ty, s);
@@ -243,8 +273,7 @@ __global__ void __launch_bounds__(THREADS) attn_fma_dkv_kernel(AttnCall C) {
   const Place p = place_of(C.seqs, C.heads_kv, false);
   if (!p.any) return;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  load_tile<T, DP>(sk, C.k, p.first, p.len, p.t0, p.head, C.dim);
-  load_tile<T, DP>(sv, C.v, p.first, p.len, p.t0, p.head, C.dim);
+  load_two<T, DP>(sk, C.k, sv, C.v, p.first, p.len, p.t0, p.head, C.dim);
   float dk[4][DP / 16], dv[4][DP / 16];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
@@ -254,8 +283,7 @@ __global__ void __launch_bounds__(THREADS) attn_fma_dkv_kernel(AttnCall C) {
     const int head = p.head * C.group + g;
     for (int i0 = C.causal ? p.t0 : 0; i0 < p.len; i0 += TILE) {
       __syncthreads();
-      load_tile<T, DP>(sq, C.q, p.first, p.len, i0, head, C.dim);
-      load_tile<T, DP>(sdo, C.d_o, p.first, p.len, i0, head, C.dim);
+      load_two<T, DP>(sq, C.q, sdo, C.d_o, p.first, p.len, i0, head, C.dim);
       float lse[4], delta[4];
       row_values(C, p, i0, head, ty, lse, delta);
       __syncthreads();
@@ -344,8 +372,6 @@ __global__ void __launch_bounds__(256) attn_rows_kernel(AttnCall C, bool wide) {
 template <typename K>
 cudaError_t run(K kernel, size_t smem, long grid, const AttnCall& c, cudaStream_t st) {
   if (grid > 0x7fffffffl) return cudaErrorInvalidValue;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (e != cudaSuccess) return e;
   kernel<<<(unsigned)grid, THREADS, smem, st>>>(c);
   return cudaGetLastError();
 }
@@ -387,6 +413,21 @@ int begin(const Attn* a, const int32_t* starts, int32_t N, int32_t total, const 
 
 }  // namespace
 
+template <typename T, int DP>
+static cudaError_t room() {
+  auto set = [](const void* k, size_t bytes) { return cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes); };
+  cudaError_t e = set((const void*)attn_fma_fwd_kernel<T, DP>, smem_of<DP>(3, 1));
+  if (e == cudaSuccess) e = set((const void*)attn_fma_dq_kernel<T, DP>, smem_of<DP>(4, 1));
+  if (e == cudaSuccess) e = set((const void*)attn_fma_dkv_kernel<T, DP>, smem_of<DP>(4, 2));
+  return e;
+}
+cudaError_t attn_fma_prepare() {
+  cudaError_t e = room<float, 64>();
+  if (e == cudaSuccess) e = room<float, 128>();
+  if (e == cudaSuccess) e = room<__nv_bfloat16, 64>();
+  if (e == cudaSuccess) e = room<__nv_bfloat16, 128>();
+  return e;
+}
 cudaError_t launch_attn_fma_fwd(const Attn* a, const AttnCall& c, cudaStream_t st) {
   if (a->desc.dtype == VCAS_DTYPE_BF16)
     return c.dim <= 64 ? fwd<__nv_bfloat16, 64>(c, st) : fwd<__nv_bfloat16, 128>(c, st);
@@ -438,6 +479,11 @@ extern "C" int vcas_attn_create(vcas_attn* out, const vcas_attn_desc* desc) {
     return VCAS_ERR_CUDA;
   }
   a->tensor_ok = d.dtype == VCAS_DTYPE_BF16 && major == 10;
+  if (attn_fma_prepare() != cudaSuccess || (a->tensor_ok && attn_umma_prepare() != cudaSuccess)) {
+    cudaGetLastError();
+    delete a;
+    return VCAS_ERR_CUDA;
+  }
   const size_t delta = ((size_t)d.heads_q * d.max_tokens * sizeof(float) + 255) & ~(size_t)255;
   a->bytes = delta + 256;
   if (cudaMalloc(&a->base, a->bytes) != cudaSuccess) {

@@ -104,10 +104,12 @@ __device__ __forceinline__ bool find_tile(const Seqs& q, int tile, int rows, int
 // No more tiles than these exist where sequences do not overlap: a sequence adds one that is not full at most.
 inline long tile_bound(int total, int N, int rows) { return total / rows + (N < total ? N : total); }
 
+cudaError_t attn_fma_prepare();
 cudaError_t launch_attn_fma_fwd(const Attn* a, const AttnCall& c, cudaStream_t st);
 cudaError_t launch_attn_fma_bwd(const Attn* a, const AttnCall& c, cudaStream_t st);
 // Zeros into dq, dk, dv on the rows of the sequences that are not worked on.
 cudaError_t launch_attn_zero(const Attn* a, const AttnCall& c, cudaStream_t st);
+cudaError_t attn_umma_prepare();         // on the current device, before the first launch there
 bool attn_umma_ok(const Attn* a, const AttnCall& c, bool backward);
 cudaError_t launch_attn_umma_fwd(const Attn* a, const AttnCall& c, cudaStream_t st);
 cudaError_t launch_attn_umma_bwd(const Attn* a, const AttnCall& c, cudaStream_t st);

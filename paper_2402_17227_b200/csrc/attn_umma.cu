@@ -236,6 +236,7 @@ __device__ __forceinline__ void end(Shared& s, const UmmaCall& P, uint32_t colum
     P.next[1] = 0;
   }
 }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* m) { asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory"); }
 // A ring position
 struct Ring {
   int stage = 0;
@@ -251,9 +252,11 @@ __device__ __forceinline__ bool take_item(Shared& s, const UmmaCall& P, int n, i
   const int lane = threadIdx.x & 31;
   volatile int* ab = &s.abort_flag;
   if (!warp_wait(&s.item_empty[n & 1], ((n >> 1) & 1) ^ 1, ab, P.c.seqs.status)) return false;
-  int at = 0;
-  if (lane == 0) at = atomicAdd(P.next, 1);
-  at = __shfl_sync(0xffffffffu, at, 0);
+  int at = (int)blockIdx.x;                          // the first one needs no counter
+  if (n > 0) {
+    if (lane == 0) at = (int)gridDim.x + atomicAdd(P.next, 1);
+    at = __shfl_sync(0xffffffffu, at, 0);
+  }
   int place = 0;
   it.first = it.len = 0;
   it.head = at % heads;
@@ -327,6 +330,11 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     Ring r;
     Item it;
     uint32_t own = 0;
+    if (lane == 0) {
+      prefetch_map(&mq);
+      prefetch_map(&mk);
+      prefetch_map(&mv);
+    }
     for (int n = 0; take_item(s, P, n, C.heads_q, C.causal, it); ++n) {
       bool ok = warp_wait(&s.own_empty, (n & 1) ^ 1, ab, status);
       if (!ok) break;
@@ -537,6 +545,13 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
     Ring r;
     Item it;
     uint32_t own = 0;
+    if (lane == 0) {
+      prefetch_map(&mq);
+      prefetch_map(&mdo);
+      prefetch_map(&mo);
+      prefetch_map(&mk);
+      prefetch_map(&mv);
+    }
     for (int n = 0; take_item(s, P, n, C.heads_q, C.causal, it); ++n) {
       bool ok = warp_wait(&s.own_empty, (n & 1) ^ 1, ab, status);
       if (!ok) break;
@@ -746,6 +761,12 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     Ring r;
     Item it;
     uint32_t own = 0;
+    if (lane == 0) {
+      prefetch_map(&mq);
+      prefetch_map(&mdo);
+      prefetch_map(&mk);
+      prefetch_map(&mv);
+    }
     for (int n = 0; take_item(s, P, n, C.heads_kv, false, it); ++n) {
       bool ok = warp_wait(&s.own_empty, (n & 1) ^ 1, ab, status);
       if (!ok) break;
@@ -941,13 +962,16 @@ bool addressable(const Strided& x, int heads, int total) {
   return ((uintptr_t)x.p & 15) == 0 && (total == 1 || (x.token % 8 == 0 && x.token > 0)) && (heads == 1 || (x.head % 8 == 0 && x.head > 0)) &&
          x.token < (1ll << 36) && x.head < (1ll << 36);
 }
+// shared memory beside the Shared struct
+template <int DC> constexpr int FWD_BYTES = DC * (CHUNK<128> + FWD_STAGES<DC> * CHUNK<FWD_TN>);
+template <int DC> constexpr int DQ_BYTES = DC * ((DC == 1 ? 3 : 2) * CHUNK<128> + BWD_STAGES<DC> * CHUNK<TN_OF<DC>>);
+template <int DC> constexpr int DKV_BYTES = DC * (2 * CHUNK<128> + BWD_STAGES<DC> * CHUNK<TN_OF<DC>>) + 2 * (TN_OF<DC> / 64) * 512;
+
 template <typename... KArgs, typename... M>
 cudaError_t run(void (*kernel)(KArgs...), bool after, int which, int bytes, int threads, int ctas, long tiles, const Attn* a,
                 const AttnCall& c, cudaStream_t st, const M&... maps) {
   if (tiles + (long)ctas * a->num_sms > 0x7fffffffl) return cudaErrorInvalidValue;       // the counter's range
   const long grid = tiles < (long)ctas * a->num_sms ? tiles : (long)ctas * a->num_sms;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes + (int)sizeof(Shared));
-  if (e != cudaSuccess) return e;
   const UmmaCall P = {c, a->next + 2 * which, a->wait_limit_ns, a->stall_once};
   return launch_maybe_after(after, kernel, dim3((unsigned)grid), dim3(threads), bytes + sizeof(Shared), st, maps..., P);
 }
@@ -961,14 +985,25 @@ cudaError_t backward(const Attn* a, const AttnCall& c, bool after, cudaStream_t 
       !attn_map(&gt, c.d_o, hq, d, total, TN) || !attn_map(&k, c.k, hk, d, total, 128) || !attn_map(&v, c.v, hk, d, total, 128))
     return cudaErrorInvalidValue;
   const long tiles = tile_bound(total, c.seqs.N, 128);
-  constexpr int OWN = DC * CHUNK<128>, RING = BWD_STAGES<DC> * DC * CHUNK<TN>;
-  const cudaError_t e = run(attn_dq_kernel<DC>, after, 1, (DC == 1 ? 3 : 2) * OWN + RING, BWD_THREADS<DC>, BWD_CTAS<DC>, tiles * hq, a, c, st, q,
-                            g, o, kt, vt);
+  const cudaError_t e = run(attn_dq_kernel<DC>, after, 1, DQ_BYTES<DC>, BWD_THREADS<DC>, BWD_CTAS<DC>, tiles * hq, a, c, st, q, g, o, kt, vt);
   if (e != cudaSuccess) return e;
-  return run(attn_dkv_kernel<DC>, true, 2, 2 * OWN + RING + 2 * (TN / 64) * 512, BWD_THREADS<DC>, BWD_CTAS<DC>, tiles * hk, a, c, st, qt, gt, k, v);
+  return run(attn_dkv_kernel<DC>, true, 2, DKV_BYTES<DC>, BWD_THREADS<DC>, BWD_CTAS<DC>, tiles * hk, a, c, st, qt, gt, k, v);
 }
 
 }  // namespace
+
+cudaError_t attn_umma_prepare() {
+  auto room = [](const void* kernel, int bytes) {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes + (int)sizeof(Shared));
+  };
+  cudaError_t e = room((const void*)attn_fwd_kernel<1>, FWD_BYTES<1>);
+  if (e == cudaSuccess) e = room((const void*)attn_fwd_kernel<2>, FWD_BYTES<2>);
+  if (e == cudaSuccess) e = room((const void*)attn_dq_kernel<1>, DQ_BYTES<1>);
+  if (e == cudaSuccess) e = room((const void*)attn_dq_kernel<2>, DQ_BYTES<2>);
+  if (e == cudaSuccess) e = room((const void*)attn_dkv_kernel<1>, DKV_BYTES<1>);
+  if (e == cudaSuccess) e = room((const void*)attn_dkv_kernel<2>, DKV_BYTES<2>);
+  return e;
+}
 
 bool attn_umma_ok(const Attn* a, const AttnCall& c, bool backward) {
   const int total = c.seqs.total;
@@ -986,8 +1021,8 @@ cudaError_t launch_attn_umma_fwd(const Attn* a, const AttnCall& c, cudaStream_t 
       !attn_map(&mv, c.v, c.heads_kv, c.dim, total, FWD_TN))
     return cudaErrorInvalidValue;
   const long tiles = tile_bound(total, c.seqs.N, 128) * c.heads_q;
-  return c.dim <= 64 ? run(attn_fwd_kernel<1>, false, 0, CHUNK<128> + FWD_STAGES<1> * CHUNK<FWD_TN>, FWD_THREADS, 2, tiles, a, c, st, mq, mk, mv)
-                     : run(attn_fwd_kernel<2>, false, 0, 2 * (CHUNK<128> + FWD_STAGES<2> * CHUNK<FWD_TN>), FWD_THREADS, 2, tiles, a, c, st, mq, mk, mv);
+  return c.dim <= 64 ? run(attn_fwd_kernel<1>, false, 0, FWD_BYTES<1>, FWD_THREADS, 2, tiles, a, c, st, mq, mk, mv)
+                     : run(attn_fwd_kernel<2>, false, 0, FWD_BYTES<2>, FWD_THREADS, 2, tiles, a, c, st, mq, mk, mv);
 }
 
 cudaError_t launch_attn_umma_bwd(const Attn* a, const AttnCall& c, cudaStream_t st) {

@@ -19,7 +19,7 @@ namespace vcas {
 namespace {
 
 constexpr int MAX_TOP = 32;
-constexpr int MAX_SLICES = 32;           // CTAs that share a row
+constexpr int MAX_SLICES = 32;           // CTAs that share a row: a lane each when they are joined
 constexpr int MAX_UNITS = 2048;          // (row, slice) pairs of a call whose rows are shared
 // values at or above the bound that a CTA of NT threads ranks; the keys of all slices of a row fit as well
 template <int NT> constexpr int CANDIDATES = NT < 64 ? 512 : MAX_SLICES * MAX_TOP;
@@ -105,6 +105,19 @@ __device__ __forceinline__ Sums join(Sums a, Sums b) {
   return a;
 }
 
+// of all lanes, in every lane
+__device__ __forceinline__ Sums join_lanes(Sums a) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    Sums b;
+    b.m = __shfl_xor_sync(0xffffffffu, a.m, o);
+    b.s = __shfl_xor_sync(0xffffffffu, a.s, o);
+    b.t = __shfl_xor_sync(0xffffffffu, a.t, o);
+    a = (threadIdx.x & o) ? join(b, a) : join(a, b);
+  }
+  return a;
+}
+
 // A value and its index as one number: larger values first, then lower indices.  -0 counts as 0.
 __device__ __forceinline__ uint64_t key_of(float x, uint32_t idx) {
   const uint32_t b = __float_as_uint(x + 0.0f);
@@ -163,6 +176,7 @@ __device__ __forceinline__ void rank_keys(const uint64_t* keys, int n, int k, F 
   for (int i = threadIdx.x; i < n; i += NT) {
     const uint64_t mine = keys[i];
     int larger = 0;
+#pragma unroll 8
     for (int j = 0; j < n; ++j) larger += keys[j] > mine;
     if (larger < k && mine != 0) f(larger, mine);
   }
@@ -303,14 +317,7 @@ __global__ void __launch_bounds__(NT) loss_fwd_kernel(FwdParams P) {
     for (int i = s.at(s.nv); i < c1; ++i) single(Vec<T>::one(row[i]), i);
 
   // the CTA's sums, in a fixed order
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    Sums b;
-    b.m = __shfl_xor_sync(0xffffffffu, a.m, o);
-    b.s = __shfl_xor_sync(0xffffffffu, a.s, o);
-    b.t = __shfl_xor_sync(0xffffffffu, a.t, o);
-    a = (threadIdx.x & o) ? join(b, a) : join(a, b);
-  }
+  a = join_lanes(a);
   if (NT > 32) {
     if ((threadIdx.x & 31) == 0) sh.sums[threadIdx.x / 32] = a;
     __syncthreads();
@@ -325,9 +332,9 @@ __global__ void __launch_bounds__(NT) loss_fwd_kernel(FwdParams P) {
     const int unit = blockIdx.x, first = (int)r * P.slices;
     if (TOP && threadIdx.x < P.top) P.keys[(size_t)unit * P.top + threadIdx.x] = sh.out[threadIdx.x];
     if (threadIdx.x == 0) P.part[unit] = make_float4(a.m, a.s, a.t, 0.f);
-    __threadfence();
     __syncthreads();
     if (threadIdx.x == 0) {
+      __threadfence();                   // for all of the CTA, which the barrier put before it
       const int done = atomicAdd(P.tickets + r, 1);
       sh.last = done == P.slices - 1;
       if (sh.last) P.tickets[r] = 0;     // for the next call
@@ -335,12 +342,14 @@ __global__ void __launch_bounds__(NT) loss_fwd_kernel(FwdParams P) {
     __syncthreads();
     if (!sh.last) return;
     __threadfence();
-    float4 f = __ldcg(P.part + first);
-    a = {f.x, f.y, f.z};
-    for (int i = 1; i < P.slices; ++i) {
-      f = __ldcg(P.part + first + i);
-      a = join(a, Sums{f.x, f.y, f.z});
+    // lane i has slice i, neighbours join first
+    const int lane = threadIdx.x & 31;
+    a = {LOWEST, 0.f, 0.f};
+    if (lane < P.slices) {
+      const float4 f = __ldcg(P.part + first + lane);
+      a = {f.x, f.y, f.z};
     }
+    a = join_lanes(a);
     if (TOP) {
       // each slice's keys are in descending order: most fall out on the slices' first ones
       const int n = P.slices * P.top;
