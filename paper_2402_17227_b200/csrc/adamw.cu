@@ -4,9 +4,12 @@
 // bytes of fp32, 16 of bf16, 8 of e4m3), and the whole table of tensors travels in the kernel's parameters, so that a step
 // neither copies a table to the device nor keeps one there.  A warp's 256 elements are the block of an 8-bit state's scale: its
 // largest value is one warp reduction, on the bits as integers, which carry a NaN along.
-// Every multiplication and addition is rounded on its own (no contraction to fma): the update is then the same to
-// the bit wherever it is computed from the formulas.
+// Every multiplication and addition is rounded on its own (no contraction to fma; two elements an instruction): with 32-bit states
+// the update is then the same to the bit wherever it is computed from the formulas.
 #include <cmath>
+
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
 
 #include "common.cuh"
 #include "vcas_train.h"
@@ -95,38 +98,89 @@ __device__ __forceinline__ void store_codes(uint8_t* p, int have, bool wide, uin
     if (i < have) p[i] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
 }
 
-// ---- e4m3: sign, four exponent bits, three of the mantissa.  Times 2^120 its exponent and mantissa are bits 20-26 of an fp32
-// value, subnormals included.
-__device__ __forceinline__ void decode(uint2 c, float scale, float (&f)[8]) {
-  const float up = 0x1p+120f;
+// ---- pairs of elements
+struct Eight { uint64_t p[4]; };
+__device__ __forceinline__ Eight pairs(const float (&f)[8]) {
+  Eight e;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t b = (i < 4 ? c.x : c.y) >> (8 * (i % 4));
-    // code * 2^120 is exact, so this is the value itself, rounded once with the scale
-    f[i] = __fmul_rn(__fmul_rn(__uint_as_float(((b & 0x7fu) << 20) | ((b & 0x80u) << 24)), up), scale);
-  }
+  for (int i = 0; i < 4; ++i) e.p[i] = pack2(f[2 * i], f[2 * i + 1]);
+  return e;
 }
-// LEAST: 1 where a positive value must not become 0
-template <uint32_t LEAST, int SHIFT>
+__device__ __forceinline__ void singles(const Eight& e, float (&f)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) unpack2(e.p[i], f[2 * i], f[2 * i + 1]);
+}
+// Products that are added to something are made one by one: mul.f32x2 in front of add.f32x2 became one fma, with a rounding less.
+__device__ __forceinline__ Eight times(const Eight& a, float by) {
+  float x[8];
+  singles(a, x);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = __fmul_rn(x[i], by);
+  return pairs(x);
+}
+// the others
+__device__ __forceinline__ Eight scaled(const Eight& a, float by) {
+  const uint64_t b = pack2(by, by);
+  Eight e;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) e.p[i] = mul2(a.p[i], b);
+  return e;
+}
+__device__ __forceinline__ Eight plus(const Eight& a, const Eight& b) {
+  Eight e;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) e.p[i] = add2(a.p[i], b.p[i]);
+  return e;
+}
+
+// ---- e4m3
+__device__ __forceinline__ Eight decode(uint2 c, float scale) {
+  float f[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t two = (i < 2 ? c.x : c.y) >> (16 * (i % 2));
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3);      // exact
+    const float2 v = __half22float2(__half2(h));
+    f[2 * i] = v.x;
+    f[2 * i + 1] = v.y;
+  }
+  return scaled(pairs(f), scale);
+}
+// A value times 2^-120 has its e4m3 exponent and mantissa in bits 20-26, subnormals included; what is below them decides together with the
+// random bits (in bits 12-19, and half of their step) whether the code goes up by one.  BYTE: of each element's halfword.
+// POSITIVE: no signs, and a positive value does not become 0.
+template <bool POSITIVE, int BYTE>
 __device__ __forceinline__ uint2 encode(const float (&f)[8], const uint32_t (&rnd)[4], float* scale_at, int lane) {
   uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
+  for (int i = 0; i < 8; ++i) top = max(top, POSITIVE ? __float_as_uint(f[i]) : __float_as_uint(f[i]) & 0x7fffffffu);
   const float big = __uint_as_float(__reduce_max_sync(0xffffffffu, top));
   if (lane == 0) *scale_at = __fmul_rn(big, 1.0f / 448.0f);
   // under 2^-100 (sqrt(v) is never that small) 448 / big would leave fp32's range: such an m is held as 0
   const float inv = big >= 0x1p-100f ? __fdiv_rn(448.0f, big) : 0.f;
   uint32_t w[2] = {0, 0};
+  float y[8], z[8];
+  singles(scaled(pairs(f), inv), y);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] = fminf(fabsf(y[i]), 448.0f);
+  singles(scaled(pairs(y), 0x1p-120f), z);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float y = fminf(__fmul_rn(fabsf(f[i]), inv), 448.0f);
-    const uint32_t r = (rnd[i / 2] >> (16 * (i % 2) + SHIFT)) & 0xffu;
-    uint32_t c = (__float_as_uint(__fmul_rn(y, 0x1p-120f)) + (r << 12) + 2048u) >> 20;
-    if (LEAST) c = f[i] > 0.f ? max(c, LEAST) : c;
-    else c |= f[i] < 0.f ? 0x80u : 0u;
-    w[i / 4] |= c << (8 * (i % 4));
+    // bytes 0, 0, random, 0x80: shifted left by 4 that is the random byte in bits 12-19 and 2048
+    const uint32_t r = __byte_perm(rnd[i / 2], 0x80u, 0x5504 | ((2 * (i % 2) + BYTE) << 4));
+    uint32_t c = __float_as_uint(z[i]) + (r << 4);
+    if (POSITIVE) c = max(c, min(__float_as_uint(f[i]), 1u << 20));
+    c <<= 4;                                         // the code in the top byte
+    if (!POSITIVE) c = (c & 0x7fffffffu) | (__float_as_uint(f[i]) & 0x80000000u);
+    w[i / 4] = __byte_perm(w[i / 4], c, 0x7321);     // and in behind those before it
   }
   return make_uint2(w[0], w[1]);
+}
+
+__device__ __forceinline__ float sqrt_fast(float x) {
+  float y;
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 
 __device__ __forceinline__ void philox(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t k0, uint32_t k1, uint32_t (&out)[4]) {
@@ -142,7 +196,7 @@ __device__ __forceinline__ void philox(uint32_t c0, uint32_t c1, uint32_t c2, ui
 }
 
 template <typename P, typename G, int BITS, int CAP>
-__global__ void __launch_bounds__(THREADS) adamw_kernel(const __grid_constant__ Table<CAP> t) {
+__global__ void __launch_bounds__(THREADS, BITS == 8 ? 6 : 4) adamw_kernel(const __grid_constant__ Table<CAP> t) {
   // the tensor this chunk belongs to: the last one that begins at or before it
   int lo = 0, hi = t.count - 1;
   while (lo < hi) {
@@ -150,67 +204,82 @@ __global__ void __launch_bounds__(THREADS) adamw_kernel(const __grid_constant__ 
     if (t.e[mid].first <= blockIdx.x) lo = mid; else hi = mid - 1;
   }
   const Entry& e = t.e[lo];
+  const int lane = threadIdx.x & 31;
+  float keep = e.keep, step_size = t.step_size, inv = t.inv, scale_g = 1.f;
+  if (t.rates != nullptr) {
+    keep = (float)(1.0 - (double)t.rates[0] * (double)e.decay);
+    step_size = t.rates[1];
+    inv = t.rates[2];
+  }
+  if (t.grad_scale != nullptr) scale_g = *t.grad_scale;
+  uint32_t k0 = t.seed_lo, k1 = t.seed_hi;
+  if (BITS == 8 && t.seed_dev != nullptr) { const uint64_t s = *t.seed_dev; k0 = (uint32_t)s; k1 = (uint32_t)(s >> 32); }
   const int64_t at = (int64_t)(blockIdx.x - e.first) * CHUNK + threadIdx.x * 8;
   const int64_t left = e.n - at;
   const int have = left >= 8 ? 8 : left > 0 ? (int)left : 0;
   // a whole warp without elements has nothing to do; the others keep all lanes for the block's largest value
   if (__all_sync(0xffffffffu, have == 0)) return;
   const bool wide = have == 8 && (e.place >> 31);
-  const int lane = threadIdx.x & 31;
-
-  float p[8], g[8], m[8], v[8];
+  const int64_t block = at >> 8;
+  float x[8], root[8];
   uint2 mc = make_uint2(0, 0), vc = make_uint2(0, 0);
   float ms = 0.f, vs = 0.f;
-  const int64_t block = at >> 8;
-  load((const G*)e.g + at, have, wide, g);
+  Eight p, g, m, v;
+  load((const G*)e.g + at, have, wide, x);
+  g = pairs(x);
   if (BITS == 32) {
-    load((const float*)e.m + at, have, wide, m);
-    load((const float*)e.v + at, have, wide, v);
+    load((const float*)e.m + at, have, wide, x);
+    m = pairs(x);
+    load((const float*)e.v + at, have, wide, x);
+    v = pairs(x);
   } else {
     mc = load_codes((const uint8_t*)e.m + at, have, wide);
     vc = load_codes((const uint8_t*)e.v + at, have, wide);
     ms = e.m_scale[block];
     vs = e.v_scale[block];
   }
-  load((const P*)e.p + at, have, wide, p);
-  float keep = e.keep, step_size = t.step_size, inv = t.inv;
-  if (t.rates != nullptr) {
-    keep = (float)(1.0 - (double)t.rates[0] * (double)e.decay);
-    step_size = t.rates[1];
-    inv = t.rates[2];
-  }
-  if (t.grad_scale != nullptr) {
-    const float s = *t.grad_scale;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) g[i] = __fmul_rn(g[i], s);
-  }
+  load((const P*)e.p + at, have, wide, x);
+  p = pairs(x);
+  if (t.grad_scale != nullptr) g = scaled(g, scale_g);
   if (BITS == 8) {
-    decode(mc, ms, m);
-    decode(vc, vs, v);
+    m = decode(mc, ms);
+    v = decode(vc, vs);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], v[i]);
+    for (int i = 0; i < 4; ++i) v.p[i] = mul2(v.p[i], v.p[i]);
   }
+  m = plus(times(m, t.b1), times(g, t.c1));
+  Eight gg;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    m[i] = __fadd_rn(__fmul_rn(m[i], t.b1), __fmul_rn(g[i], t.c1));
-    v[i] = __fadd_rn(__fmul_rn(v[i], t.b2), __fmul_rn(__fmul_rn(g[i], g[i]), t.c2));
-    const float root = __fsqrt_rn(v[i]);
-    const float denom = __fadd_rn(__fmul_rn(root, inv), t.eps);
-    p[i] = __fadd_rn(__fmul_rn(p[i], keep), -__fdiv_rn(__fmul_rn(m[i], step_size), denom));
-    if (BITS == 8) v[i] = root;
-  }
-  store((P*)e.p + at, have, wide, p);
-  if (sizeof(P) == 4 && e.copy != nullptr) store((__nv_bfloat16*)e.copy + at, have, wide, p);
+  for (int i = 0; i < 4; ++i) gg.p[i] = mul2(g.p[i], g.p[i]);
+  v = plus(times(v, t.b2), times(gg, t.c2));
+  singles(v, root);
+  // 32-bit states: the correctly rounded root and quotient, which HBM leaves time for.  8-bit ones, with half the bytes, do not
+  // (314 M elements: 1266 us): there both are good to an ulp or two.
+#pragma unroll
+  for (int i = 0; i < 8; ++i) root[i] = BITS == 32 ? __fsqrt_rn(root[i]) : sqrt_fast(root[i]);
+  float denom[8], step[8];
+  const uint64_t eps = pack2(t.eps, t.eps);
+  Eight d = times(pairs(root), inv);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) d.p[i] = add2(d.p[i], eps);
+  singles(d, denom);
+  singles(scaled(m, step_size), step);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) step[i] = -(BITS == 32 ? __fdiv_rn(step[i], denom[i]) : __fdividef(step[i], denom[i]));
+  singles(plus(times(p, keep), pairs(step)), x);
+  store((P*)e.p + at, have, wide, x);
+  if (sizeof(P) == 4 && e.copy != nullptr) store((__nv_bfloat16*)e.copy + at, have, wide, x);
+  singles(m, x);
   if (BITS == 32) {
-    store((float*)e.m + at, have, wide, m);
-    store((float*)e.v + at, have, wide, v);
+    store((float*)e.m + at, have, wide, x);
+    singles(v, x);
+    store((float*)e.v + at, have, wide, x);
   } else {
     // elements behind the tensor's end count as zeros (0 / (0 + eps) leaves m and r at 0)
-    uint32_t k0 = t.seed_lo, k1 = t.seed_hi, rnd[4];
-    if (t.seed_dev != nullptr) { const uint64_t s = *t.seed_dev; k0 = (uint32_t)s; k1 = (uint32_t)(s >> 32); }
+    uint32_t rnd[4];
     philox((uint32_t)(at >> 3), e.place & 0x7fffffffu, 3u, k0, k1, rnd);
-    const uint2 mo = encode<0, 0>(m, rnd, e.m_scale + block, lane);
-    const uint2 vo = encode<1, 8>(v, rnd, e.v_scale + block, lane);
+    const uint2 mo = encode<false, 0>(x, rnd, e.m_scale + block, lane);
+    const uint2 vo = encode<true, 1>(root, rnd, e.v_scale + block, lane);
     store_codes((uint8_t*)e.m + at, have, wide, mo);
     store_codes((uint8_t*)e.v + at, have, wide, vo);
   }
