@@ -92,23 +92,20 @@ __device__ __forceinline__ void load_tile(uint8_t* dst, const CUtensorMap* map, 
 #pragma unroll
   for (int c = 0; c < DC; ++c) tma_load_3d(dst + c * CHUNK<ROWS>, map, 64 * c, head, token, bar);
 }
-// sum over a row of two tiles of 128 rows of their products
-template <int DC>
+// sum over 64 columns of a row of two tiles of their products
 __device__ __forceinline__ float row_dot(const uint8_t* a, const uint8_t* b, int row) {
   float s0 = 0.f, s1 = 0.f;
 #pragma unroll
-  for (int c = 0; c < DC; ++c)
+  for (int v = 0; v < 8; ++v) {
+    const int at = row * 128 + ((v ^ (row & 7)) << 4);           // the 128-byte swizzle
+    const uint4 x = *reinterpret_cast<const uint4*>(a + at), y = *reinterpret_cast<const uint4*>(b + at);
+    const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-    for (int v = 0; v < 8; ++v) {
-      const int at = c * CHUNK<128> + row * 128 + ((v ^ (row & 7)) << 4);          // the 128-byte swizzle
-      const uint4 x = *reinterpret_cast<const uint4*>(a + at), y = *reinterpret_cast<const uint4*>(b + at);
-      const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        s0 = fmaf(__uint_as_float(xs[e] << 16), __uint_as_float(ys[e] << 16), s0);
-        s1 = fmaf(__uint_as_float(xs[e] & 0xffff0000u), __uint_as_float(ys[e] & 0xffff0000u), s1);
-      }
+    for (int e = 0; e < 4; ++e) {
+      s0 = fmaf(__uint_as_float(xs[e] << 16), __uint_as_float(ys[e] << 16), s0);
+      s1 = fmaf(__uint_as_float(xs[e] & 0xffff0000u), __uint_as_float(ys[e] & 0xffff0000u), s1);
     }
+  }
   return s0 + s1;
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -527,7 +524,8 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
   static_assert(!O_IN_RING || TN == 128, "as large as a tile of the ring");
   extern __shared__ __align__(1024) uint8_t smem[];
   uint8_t *sq = smem, *sdo = sq + OWN, *so = sdo + OWN, *ring = O_IN_RING ? so : so + OWN;
-  Shared& s = *reinterpret_cast<Shared*>(ring + STAGES * TILE);
+  float* s_half = reinterpret_cast<float*>(ring + STAGES * TILE);    // [DC][128] parts of delta
+  Shared& s = *reinterpret_cast<Shared*>(s_half + DC * 128);
   const AttnCall& C = P.c;
   if (!in_place(smem, C.seqs.status)) return;
   // The kernel before it may be the one that writes zeros to the other sequences' rows, which runs beside this one (it has begun, so
@@ -584,39 +582,43 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
       const int tiles = tiles_of(it);
       ok = warp_wait(&s.own_full, n & 1, ab, status);
       if (!ok) break;
-      int k_now = 0, k_next = 0, v_next = 0;         // ring places of this tile's K, and of the next one's K and V
-      // waits for K and V of tile j and multiplies K with Q
-      auto scores = [&](int j) {
-        const int have = it.len - j * TN;
-        for (int x = 0; x < 2 && ok; ++x) {
-          ok = warp_wait(&s.full[r.stage], r.phase, ab, status);
-          if (ok && have < TN) zero_rows<DC, TN>(ring + r.stage * TILE, have, lane);
-          (x == 0 ? k_next : v_next) = r.stage;
-          r.next(STAGES);
-        }
-        if (!ok) return;
-        if (have < TN) {
+      int k_now = 0, k_next = 0;         // ring places of this tile's K and the next one's
+      // waits for the next tile of the ring; rows behind the sequence's end become 0
+      auto arrived = [&](int j) {
+        const int place = r.stage, have = it.len - j * TN;
+        ok = warp_wait(&s.full[place], r.phase, ab, status);
+        if (ok && have < TN) {
+          zero_rows<DC, TN>(ring + place * TILE, have, lane);
           fence_async_smem();
           __syncwarp();
         }
+        r.next(STAGES);
         tc_fence_after();
+        return place;
+      };
+      auto scores = [&](int j) {
+        k_next = arrived(j);
+        if (!ok) return;
         if (leader) {
           product_tiles<DC, TN>(ts + (score & 1) * TN, smem_u32(sq), smem_u32(ring + k_next * TILE));
           umma_commit(&s.scores[score & 1]);
         }
         ++score;
       };
-      auto dscores = [&](bool last) {
+      auto dscores = [&](int j) {
+        const int v = arrived(j);
+        if (!ok) return;
         if (leader) {
-          product_tiles<DC, TN>(tdp, smem_u32(sdo), smem_u32(ring + v_next * TILE));
+          product_tiles<DC, TN>(tdp, smem_u32(sdo), smem_u32(ring + v * TILE));
           umma_commit(&s.dscores);
-          umma_commit(&s.empty[v_next]);
-          if (last) umma_commit(&s.own_empty);
+          umma_commit(&s.empty[v]);
+          if (j == tiles - 1) umma_commit(&s.own_empty);
         }
       };
       scores(0);
       if (!ok) break;
-      dscores(tiles == 1);
+      dscores(0);
+      if (!ok) break;
       if (O_IN_RING) {
         // O's place is given back when the other warps have read it
         ok = warp_wait(&s.o_read, n & 1, ab, status);
@@ -634,7 +636,8 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         ok = ok && warp_wait(&s.ready[0], made & 1, ab, status);
         if (!ok) break;
         tc_fence_after();
-        if (j + 1 < tiles) dscores(j + 2 == tiles);
+        if (j + 1 < tiles) dscores(j + 1);
+        if (!ok) break;
         if (leader) {
           product_rows<DC, TN, 0, TN / 16>(tdq, ts + (made & 1) * TN, 64, smem_u32(ring + k_now * TILE), j != 0);
           umma_commit(&s.empty[k_now]);
@@ -668,10 +671,17 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         r.next(STAGES);
         for (int i = 2; i < 2 * tiles; ++i) r.next(STAGES);
       }
-      // by all warps that need it; the dK, dV kernel reads it
-      const float delta = row_dot<DC>(sdo, o_tile, in);
-      if (O_IN_RING) warp_arrive(&s.o_read);
+      // a warp sums over 64 columns; the dK, dV kernel reads delta
+      static_assert(WARPS == 4 * DC, "every 64 columns have a warp");
+      float delta = row_dot(sdo + part * CHUNK<128>, o_tile + part * CHUNK<128>, in);
+      if (DC == 2) s_half[part * 128 + in] = delta;
+      warp_arrive(&s.o_read);
       warp_arrive(&s.own_empty);
+      if (DC == 2) {
+        ok = warp_wait(&s.o_read, n & 1, ab, status);
+        if (!ok) break;
+        delta = s_half[in] + s_half[128 + in];
+      }
       if (part == 0 && row < it.len) C.delta[at_row] = delta;
       const uint64_t n2 = pack2(-lse, -lse), d2 = pack2(-delta, -delta);
       for (int j = 0; j < tiles; ++j, ++made) {
@@ -688,12 +698,15 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
           a[2 * i] = __float_as_uint(attn_exp2(e0));
           a[2 * i + 1] = __float_as_uint(attn_exp2(e1));
         }
+        const int see = min(TN, (C.causal ? min(it.len, row + 1) : it.len) - j * TN) - part * 64;
+        if (__any_sync(0xffffffffu, see < 64)) {
+#pragma unroll
+          for (int i = 0; i < 64; ++i) a[i] = i < see ? a[i] : 0u;
+        }
         ok = warp_wait(&s.dscores, made & 1, ab, status);
         if (!ok) break;
         tc_fence_after();
         uint32_t o[32];
-        const int see = min(TN, (C.causal ? min(it.len, row + 1) : it.len) - j * TN) - part * 64;
-        const bool whole = !__any_sync(0xffffffffu, see < 64);
         {
           uint32_t b[64];
           tmem_ld64(tdp + lanes + part * 64, b);
@@ -702,10 +715,6 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             float s0, s1;
             unpack2(mul2(pack2(__uint_as_float(a[2 * i]), __uint_as_float(a[2 * i + 1])),
                          add2(pack2(__uint_as_float(b[2 * i]), __uint_as_float(b[2 * i + 1])), d2)), s0, s1);
-            if (!whole) {
-              s0 = 2 * i < see ? s0 : 0.f;
-              s1 = 2 * i + 1 < see ? s1 : 0.f;
-            }
             o[i] = pack_bf16(s0, s1);
           }
         }
@@ -717,7 +726,6 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
       ok = ok && warp_wait(&s.done, n & 1, ab, status);
       if (!ok) break;
       // a warp stores 64 columns
-      static_assert(WARPS == 4 * DC, "every column has a warp");
       tc_fence_after();
       Strided x = C.dq;
       x.p = (const __nv_bfloat16*)x.p + part * 64;
@@ -796,26 +804,29 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
       ok = warp_wait(&s.own_full, n & 1, ab, status);
       if (!ok) break;
       int q_next = 0, g_next = 0;        // ring places of the next step's Q and dO
-      auto scores = [&](int i) {
-        const int have = it.len - step_of(it, i, per).row;
-        for (int x = 0; x < 2 && ok; ++x) {
-          ok = warp_wait(&s.full[r.stage], r.phase, ab, status);
-          if (ok && have < TN) zero_rows<DC, TN>(ring + r.stage * TILE, have, lane);
-          (x == 0 ? q_next : g_next) = r.stage;
-          r.next(STAGES);
-        }
-        if (!ok) return;
-        if (have < TN) {
+      auto arrived = [&](int i) {
+        const int place = r.stage, have = it.len - step_of(it, i, per).row;
+        ok = warp_wait(&s.full[place], r.phase, ab, status);
+        if (ok && have < TN) {
+          zero_rows<DC, TN>(ring + place * TILE, have, lane);
           fence_async_smem();
           __syncwarp();
         }
+        r.next(STAGES);
         tc_fence_after();
+        return place;
+      };
+      auto scores = [&](int i) {
+        q_next = arrived(i);
+        if (!ok) return;
         if (leader) {
           product_tiles<DC, TN>(ts, smem_u32(sk), smem_u32(ring + q_next * TILE));
           umma_commit(&s.scores[0]);
         }
       };
       auto dscores = [&](int i) {
+        g_next = arrived(i);
+        if (!ok) return;
         if (leader) {
           product_tiles<DC, TN>(tdp, smem_u32(sv), smem_u32(ring + g_next * TILE));
           umma_commit(&s.dscores);
@@ -825,6 +836,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
       scores(0);
       if (!ok) break;
       dscores(0);
+      if (!ok) break;
       for (int i = 0; i < steps; ++i, ++made) {
         if (i == 0) ok = warp_wait(&s.acc_empty, (n & 1) ^ 1, ab, status);
         ok = ok && warp_wait(&s.ready[0], made & 1, ab, status);
@@ -848,6 +860,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
           if (i == steps - 1) umma_commit(&s.done);
         }
         if (i + 1 < steps) dscores(i + 1);
+        if (!ok) break;
       }
     }
     if (leader && *ab) drain_products(&s.drain, ab, status);
@@ -893,17 +906,16 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
             const int x = 2 * (e + h);
             float e0, e1;
             unpack2(fma2(pack2(__uint_as_float(a[x]), __uint_as_float(a[x + 1])), c2, h == 0 ? pack2(f.x, f.y) : pack2(f.z, f.w)), e0, e1);
-            e0 = attn_exp2(e0);
-            e1 = attn_exp2(e1);
-            if (cut) {
-              e0 = x >= lo && x < hi ? e0 : 0.f;
-              e1 = x + 1 >= lo && x + 1 < hi ? e1 : 0.f;
-            }
-            a[x] = __float_as_uint(e0);
-            a[x + 1] = __float_as_uint(e1);
-            o[e + h] = pack_bf16(e0, e1);
+            a[x] = __float_as_uint(attn_exp2(e0));
+            a[x + 1] = __float_as_uint(attn_exp2(e1));
           }
         }
+        if (cut) {
+#pragma unroll
+          for (int x = 0; x < 64; ++x) a[x] = x >= lo && x < hi ? a[x] : 0u;
+        }
+#pragma unroll
+        for (int e = 0; e < 32; ++e) o[e] = pack_bf16(__uint_as_float(a[2 * e]), __uint_as_float(a[2 * e + 1]));
         tmem_st32(ts + lanes + part * 64, o);
         tmem_wait_st();
         tc_fence_before();
@@ -964,7 +976,7 @@ bool addressable(const Strided& x, int heads, int total) {
 }
 // shared memory beside the Shared struct
 template <int DC> constexpr int FWD_BYTES = DC * (CHUNK<128> + FWD_STAGES<DC> * CHUNK<FWD_TN>);
-template <int DC> constexpr int DQ_BYTES = DC * ((DC == 1 ? 3 : 2) * CHUNK<128> + BWD_STAGES<DC> * CHUNK<TN_OF<DC>>);
+template <int DC> constexpr int DQ_BYTES = DC * ((DC == 1 ? 3 : 2) * CHUNK<128> + BWD_STAGES<DC> * CHUNK<TN_OF<DC>> + 512);
 template <int DC> constexpr int DKV_BYTES = DC * (2 * CHUNK<128> + BWD_STAGES<DC> * CHUNK<TN_OF<DC>>) + 2 * (TN_OF<DC> / 64) * 512;
 
 template <typename... KArgs, typename... M>
