@@ -95,7 +95,7 @@ __device__ __forceinline__ void load_tile(uint8_t* dst, const CUtensorMap* map, 
 // sum over 64 columns of a row of two tiles of their products
 __device__ __forceinline__ float row_dot(const uint8_t* a, const uint8_t* b, int row) {
   float s0 = 0.f, s1 = 0.f;
-#pragma unroll
+#pragma unroll 2
   for (int v = 0; v < 8; ++v) {
     const int at = row * 128 + ((v ^ (row & 7)) << 4);           // the 128-byte swizzle
     const uint4 x = *reinterpret_cast<const uint4*>(a + at), y = *reinterpret_cast<const uint4*>(b + at);
@@ -243,9 +243,10 @@ struct Ring {
     if (++stage == stages) { stage = 0; phase ^= 1u; }
   }
 };
-// The loading warp's part: takes the next tile off the counter and tells the others.  The counter goes through the heads first, then
-// through the tiles of a sequence (last_first: from its end), so that CTAs at work at the same time share the other side's tiles.
-__device__ __forceinline__ bool take_item(Shared& s, const UmmaCall& P, int n, int heads, bool last_first, Item& it) {
+// The loading warp's part: takes the next tile off the counter and tells the others.  The counter goes through the heads first, so that
+// CTAs at work at the same time share the other side's tiles, then through the tiles in the order of `Order`.
+// With lse, [2][128] floats of shared memory, the rows' lse comes along (a load of their own, at the start of a tile, was 1100 cycles).
+__device__ __forceinline__ bool take_item(Shared& s, const UmmaCall& P, const Order& order, int n, int heads, Item& it, float* lse = nullptr) {
   const int lane = threadIdx.x & 31;
   volatile int* ab = &s.abort_flag;
   if (!warp_wait(&s.item_empty[n & 1], ((n >> 1) & 1) ^ 1, ab, P.c.seqs.status)) return false;
@@ -257,18 +258,22 @@ __device__ __forceinline__ bool take_item(Shared& s, const UmmaCall& P, int n, i
   int place = 0;
   it.first = it.len = 0;
   it.head = at % heads;
-  it.any = find_tile(P.c.seqs, at / heads, 128, lane, it.first, it.len, place);
-  it.t0 = (last_first ? (it.len + 127) / 128 - 1 - place : place) * 128;
-  if (lane == 0) {
-    s.item[n & 1] = it;
-    mbar_arrive(&s.item_full[n & 1]);
+  it.any = order.find(P.c.seqs, at / heads, lane, it.first, it.len, place);
+  it.t0 = place * 128;
+  if (lse != nullptr && it.any) {
+    const float* from = P.c.lse + (int64_t)it.head * P.c.seqs.total + it.first + it.t0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) lse[(n & 1) * 128 + 32 * i + lane] = it.t0 + 32 * i + lane < it.len ? __ldcg(from + 32 * i + lane) : 0.f;
   }
+  if (lane == 0) s.item[n & 1] = it;
+  warp_arrive(&s.item_full[n & 1]);
   return it.any;
 }
-// The others' part.  False: no more, or given up.
-__device__ __forceinline__ bool get_item(Shared& s, int n, int32_t* status, Item& it) {
+// The others' part.  False: no more, or given up.  lse: of one row of the tile.
+__device__ __forceinline__ bool get_item(Shared& s, int n, int32_t* status, Item& it, const float* lse = nullptr, float* mine = nullptr) {
   if (!warp_wait(&s.item_full[n & 1], (n >> 1) & 1, &s.abort_flag, status)) return false;
   it = s.item[n & 1];
+  if (lse != nullptr) *mine = lse[(n & 1) * 128];
   warp_arrive(&s.item_empty[n & 1]);
   return it.any;
 }
@@ -324,6 +329,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
   auto tiles_of = [&](const Item& it) { return ((C.causal ? min(it.len, it.t0 + 128) : it.len) + TN - 1) / TN; };
 
   if (warp == 5) {
+    const Order order(C.seqs, lane, C.causal, false);
     Ring r;
     Item it;
     uint32_t own = 0;
@@ -332,7 +338,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
       prefetch_map(&mk);
       prefetch_map(&mv);
     }
-    for (int n = 0; take_item(s, P, n, C.heads_q, C.causal, it); ++n) {
+    for (int n = 0; take_item(s, P, order, n, C.heads_q, it); ++n) {
       bool ok = warp_wait(&s.own_empty, (n & 1) ^ 1, ab, status);
       if (!ok) break;
       if (elect_one()) {
@@ -525,7 +531,8 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
   extern __shared__ __align__(1024) uint8_t smem[];
   uint8_t *sq = smem, *sdo = sq + OWN, *so = sdo + OWN, *ring = O_IN_RING ? so : so + OWN;
   float* s_half = reinterpret_cast<float*>(ring + STAGES * TILE);    // [DC][128] parts of delta
-  Shared& s = *reinterpret_cast<Shared*>(s_half + DC * 128);
+  float* s_lse = s_half + DC * 128;                                  // [2][128]
+  Shared& s = *reinterpret_cast<Shared*>(s_lse + 2 * 128);
   const AttnCall& C = P.c;
   if (!in_place(smem, C.seqs.status)) return;
   // The kernel before it may be the one that writes zeros to the other sequences' rows, which runs beside this one (it has begun, so
@@ -540,6 +547,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
   auto tiles_of = [&](const Item& it) { return ((C.causal ? min(it.len, it.t0 + 128) : it.len) + TN - 1) / TN; };
 
   if (warp == WARPS + 1) {
+    const Order order(C.seqs, lane, C.causal, false);
     Ring r;
     Item it;
     uint32_t own = 0;
@@ -550,7 +558,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
       prefetch_map(&mk);
       prefetch_map(&mv);
     }
-    for (int n = 0; take_item(s, P, n, C.heads_q, C.causal, it); ++n) {
+    for (int n = 0; take_item(s, P, order, n, C.heads_q, it, s_lse); ++n) {
       bool ok = warp_wait(&s.own_empty, (n & 1) ^ 1, ab, status);
       if (!ok) break;
       const int token = it.first + it.t0;
@@ -655,10 +663,11 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
     uint32_t made = 0;
     Ring r;                              // the loads, to find O among them
     bool ok = true;
-    for (int n = 0; ok && get_item(s, n, status, it); ++n) {
-      const int tiles = tiles_of(it), in = (warp & 3) * 32 + lane, row = it.t0 + in;
+    float lse = 0.f;
+    const int in = (warp & 3) * 32 + lane;
+    for (int n = 0; ok && get_item(s, n, status, it, s_lse + in, &lse); ++n) {
+      const int tiles = tiles_of(it), row = it.t0 + in;
       const int64_t at_row = (int64_t)it.head * C.seqs.total + it.first + row;
-      const float lse = row < it.len ? __ldcg(C.lse + at_row) * ATTN_LOG2E : 0.f;
       ok = warp_wait(&s.own_full, n & 1, ab, status);
       if (!ok) break;
       const uint8_t* o_tile = so;
@@ -683,7 +692,8 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         delta = s_half[in] + s_half[128 + in];
       }
       if (part == 0 && row < it.len) C.delta[at_row] = delta;
-      const uint64_t n2 = pack2(-lse, -lse), d2 = pack2(-delta, -delta);
+      const float nl = -lse * ATTN_LOG2E;
+      const uint64_t n2 = pack2(nl, nl), d2 = pack2(-delta, -delta);
       for (int j = 0; j < tiles; ++j, ++made) {
         ok = warp_wait(&s.scores[made & 1], (made >> 1) & 1, ab, status);
         if (!ok) break;
@@ -766,6 +776,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
   auto step_of = [&](const Item& it, int i, int per) { return Step{it.head * C.group + i / per, (first_tile(it) + i % per) * TN}; };
 
   if (warp == WARPS + 1) {
+    const Order order(C.seqs, lane, C.causal, true);
     Ring r;
     Item it;
     uint32_t own = 0;
@@ -775,7 +786,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
       prefetch_map(&mk);
       prefetch_map(&mv);
     }
-    for (int n = 0; take_item(s, P, n, C.heads_kv, false, it); ++n) {
+    for (int n = 0; take_item(s, P, order, n, C.heads_kv, it); ++n) {
       bool ok = warp_wait(&s.own_empty, (n & 1) ^ 1, ab, status);
       if (!ok) break;
       if (elect_one()) {
@@ -879,10 +890,10 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         const Step st = step_of(it, i, per);
         const int t = st.row + part * 64 + (warp & 3) * 16 + (lane & 15);
         const int64_t at = (int64_t)st.head * C.seqs.total + it.first + t;
-        return t >= it.len ? 0.f : lane < 16 ? -C.lse[at] * ATTN_LOG2E : -C.delta[at];
+        return t >= it.len ? 0.f : lane < 16 ? C.lse[at] : C.delta[at];
       };
       auto keep = [&](uint32_t k, float f) {
-        s_rows[((k & 1) * (TN / 64) + part) * 128 + (lane >> 4) * 64 + (warp & 3) * 16 + (lane & 15)] = f;
+        s_rows[((k & 1) * (TN / 64) + part) * 128 + (lane >> 4) * 64 + (warp & 3) * 16 + (lane & 15)] = lane < 16 ? -f * ATTN_LOG2E : -f;
         warp_arrive(&s.rows_full[part][k & 1]);
       };
       keep(made, fetch(0));
@@ -949,11 +960,10 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
       if (!ok) break;
       // with eight warps one half stores dV, the other dK
       tc_fence_after();
-      auto store = [&](const Strided& x, uint32_t from, float f) {
-        store_rows<DC>(from + lanes, x, (int64_t)it.first + warp_row, it.head, C.dim, it.len - warp_row, f);
-      };
-      if (WARPS == 4 || part == 0) store(C.dv, tdv, 1.0f);
-      if (WARPS == 4 || part == 1) store(C.dk, tdk, C.scale);
+#pragma unroll 1
+      for (int which = WARPS == 4 ? 0 : part; which < (WARPS == 4 ? 2 : part + 1); ++which)
+        store_rows<DC>((which == 0 ? tdv : tdk) + lanes, which == 0 ? C.dv : C.dk, (int64_t)it.first + warp_row, it.head, C.dim,
+                       it.len - warp_row, which == 0 ? 1.0f : C.scale);
       tc_fence_before();
       warp_arrive(&s.acc_empty);
     }
@@ -976,7 +986,7 @@ bool addressable(const Strided& x, int heads, int total) {
 }
 // shared memory beside the Shared struct
 template <int DC> constexpr int FWD_BYTES = DC * (CHUNK<128> + FWD_STAGES<DC> * CHUNK<FWD_TN>);
-template <int DC> constexpr int DQ_BYTES = DC * ((DC == 1 ? 3 : 2) * CHUNK<128> + BWD_STAGES<DC> * CHUNK<TN_OF<DC>> + 512);
+template <int DC> constexpr int DQ_BYTES = DC * ((DC == 1 ? 3 : 2) * CHUNK<128> + BWD_STAGES<DC> * CHUNK<TN_OF<DC>> + 512) + 1024;
 template <int DC> constexpr int DKV_BYTES = DC * (2 * CHUNK<128> + BWD_STAGES<DC> * CHUNK<TN_OF<DC>>) + 2 * (TN_OF<DC> / 64) * 512;
 
 template <typename... KArgs, typename... M>
