@@ -464,7 +464,7 @@ class Attention(_Handle):
     def __init__(self, max_tokens: int, max_seqs: int, heads_q: int, heads_kv: int, head_dim: int,
                  dtype: torch.dtype = torch.bfloat16, causal: bool = False, scale: float = 0.0):
         _need(dtype in _DTYPES, "attention is in bfloat16 or float32")
-        self.heads_q, self.heads_kv, self.head_dim, self.dtype = heads_q, heads_kv, head_dim, dtype
+        self.heads_q, self.heads_kv, self.head_dim, self.dtype, self.causal = heads_q, heads_kv, head_dim, dtype, bool(causal)
         self._create(AttnDesc(max_tokens, max_seqs, heads_q, heads_kv, head_dim, _DTYPES[dtype], 1 if causal else 0, scale))
         # the tensors of a call as the library takes them: filled anew by every call (d_o, q, k, v, o, dq, dk, dv)
         self._args = [AttnTensor() for _ in range(8)]

@@ -1,4 +1,5 @@
-"""Backward pass through a stack of linear layers with the chain entry point (vcas_linear_bwd_chain).
+"""Backward pass through a stack of linear layers with the chain entry point (vcas_linear_bwd_chain), from a loss over
+tokens, through the attention between two of them, to the optimizer step.
 
 Orchestration only: which layer hands what to the next one.  Going down the stack (the order of
 backpropagation) every layer receives the list of data the layer above kept - all other data have an
@@ -16,10 +17,45 @@ from . import binding as vb
 
 
 @dataclass
+class TokenLossInput:
+    """The loss on top of a stack: what the forward pass left for its gradient, one of each per batch variant.
+
+    logits: [R, vocab] (rows may be padded); tokens: [R], negative where there is none; g_logp, g_entropy: the loss's
+    derivatives by logp and entropy ([R] float32; -1/R for a mean cross-entropy)."""
+    op: vb.TokenLoss
+    logits: list
+    tokens: list
+    lse: list
+    g_logp: list
+    entropy: list | None = None
+    g_entropy: list | None = None
+
+
+@dataclass
+class AttentionInput:
+    """An attention between two layers of a stack: q, k and v as the layer under it made them, side by side in [R, heads_q +
+    2 heads_kv, head_dim], and what its forward pass left, one of each per batch variant.  starts: int32 [N + 1], the N data."""
+    op: vb.Attention
+    qkv: list
+    o: list
+    lse: list
+    starts: torch.Tensor
+
+    def split(self, x):
+        """q, k and v (or their gradients) in a [R, heads_q + 2 heads_kv, head_dim] buffer."""
+        hq, hk = self.op.heads_q, self.op.heads_kv
+        return x[:, :hq], x[:, hq:hq + hk], x[:, hq + hk:]
+
+
+@dataclass
 class StackLayer:
     """One linear layer of the stack, in backward order.
 
     chained: this layer's dY is the dX of the layer before it in backward order.
+    attention: this layer's dY is the gradient of an attention whose output is the input of the layer before it in backward
+    order.
+    loss: this layer's dY is the gradient of a loss over tokens (the first layer in backward order); d_out may exceed the
+    vocabulary, the gradient is 0 there.
     H: pre-activation of a GELU feeding THIS layer's input; its dX is multiplied by GELU'(H) (App. E)."""
     name: str
     d_in: int
@@ -29,12 +65,16 @@ class StackLayer:
     dY: list           # incoming gradients per batch variant [R, d_out] (unused when chained)
     H: list | None = None      # pre-activation of the GELU feeding this layer's input, per variant [R, d_in]
     chained: bool = False
+    attention: AttentionInput | None = None
+    loss: TokenLossInput | None = None
     handle: vb.Layer | None = None
     kept: torch.Tensor | None = None
     kept_cnt: torch.Tensor | None = None
     a_out: torch.Tensor | None = None
     dX: torch.Tensor | None = None
     dW: torch.Tensor | None = None
+    grad: torch.Tensor | None = None       # dY of a layer with attention or loss
+    norms: torch.Tensor | None = None      # its rows' square-norms, from the loss
 
 
 class LinearStack:
@@ -63,6 +103,16 @@ class LinearStack:
             L.kept = torch.zeros(N, dtype=torch.int32, device=dev)
             L.kept_cnt = torch.zeros(1, dtype=torch.int32, device=dev)
             L.dW = torch.empty(L.d_out, L.d_in, dtype=torch.float32, device=dev)
+            assert (L.loss is None or i == 0) and (L.attention is None or i > 0) and \
+                sum((L.chained, L.attention is not None, L.loss is not None)) <= 1, "one source of a layer's dY"
+            if L.attention is not None:
+                a = L.attention.op
+                assert layers[i - 1].d_in == a.heads_q * a.head_dim and L.d_out == (a.heads_q + 2 * a.heads_kv) * a.head_dim
+                L.grad = torch.empty(self.R, L.d_out, dtype=dtype, device=dev)
+            if L.loss is not None:
+                assert L.loss.op.vocab <= L.d_out
+                L.grad = torch.zeros(self.R, L.d_out, dtype=dtype, device=dev)
+                L.norms = torch.empty(self.R, dtype=torch.float32, device=dev)
             nxt = layers[i + 1] if i + 1 < len(layers) else None
             if nxt is not None and nxt.chained:
                 assert nxt.d_out == L.d_in, "a chained layer's dY is the previous layer's dX"
@@ -85,14 +135,20 @@ class LinearStack:
             kw = {}
             if prev is not None:
                 kw.update(alive_in=prev.kept, alive_cnt_in=prev.kept_cnt)
+            if hook is not None:
+                hook(i, L, False)
             if L.chained:
                 dY = prev.dX
                 kw.update(a_in=prev.a_out, a_in_parts=prev.handle.chain_parts())
+            elif L.attention is not None:
+                dY = self._attention_grad(L, prev, v, alive_in=prev.kept, alive_cnt_in=prev.kept_cnt,
+                                          skip_dropped_rows=self.skip_dropped_rows)
+            elif L.loss is not None:
+                dY = self._loss_grad(L, v)
+                kw.update(a_in=L.norms, a_in_parts=1)
             else:
                 dY = L.dY[v]
             H = L.H[v % len(L.H)] if L.H is not None else None
-            if hook is not None:
-                hook(i, L, False)
             L.handle.linear_bwd_chain(L.X[v], dY, L.W, float(rho[i]), float(nu[i]), seed * len(self.layers) + i,
                                       L.dX, L.dW, H=H, a_out=L.a_out, kept_out=L.kept, kept_cnt_out=L.kept_cnt,
                                       skip_dropped_rows=self.skip_dropped_rows, defer_join=self.overlap_layers, **kw)
@@ -103,15 +159,45 @@ class LinearStack:
             for h in self.handles.values():
                 h.join()
 
+    def _attention_grad(self, L: StackLayer, prev: StackLayer, v: int, **kept):
+        """dY of the layer under an attention from the dX of the layer above it; of the kept data only, where they are given."""
+        a = L.attention
+        q, k, vv = a.split(a.qkv[v])
+        dq, dk, dv = a.split(L.grad.view(self.R, -1, a.op.head_dim))
+        a.op.bwd(prev.dX.view(a.o[v].shape), q, k, vv, a.o[v], a.lse[v], a.starts, dq=dq, dk=dk, dv=dv, **kept)
+        return L.grad
+
+    def _loss_grad(self, L: StackLayer, v: int):
+        """dY of the top layer, and its rows' square-norms."""
+        o = L.loss
+        o.op.bwd(o.logits[v], o.tokens[v], o.lse[v], o.g_logp[v], entropy=o.entropy[v] if o.entropy else None,
+                 g_entropy=o.g_entropy[v] if o.g_entropy else None, dlogits=L.grad[:, :o.op.vocab], a_out=L.norms)
+        return L.grad
+
+    def make_optimizer(self, bits: int = 32, weight_decay: float = 0.0) -> vb.AdamW:
+        """AdamW over the stack's weights from their dW, in one launch: fp32 weights in place; bf16 ones from fp32 masters that the
+        optimizer holds (its `tensors[i].p`), the bf16 weights being the copy that each step writes.  bits: of the states."""
+        entries = []
+        for L in self.layers:
+            low = L.W.dtype == torch.bfloat16
+            entries.append(vb.AdamWTensor.make(L.W.float() if low else L.W, L.dW, bits, copy=L.W if low else None,
+                                               weight_decay=weight_decay))
+        return vb.AdamW(entries)
+
     def dense_backward(self, variant: int = 0, hook=None) -> None:
         """The exact backward of the same layers (no sampling; the GELU Jacobian where the sampled pass has it):
         the dense comparison."""
         prev = None
         for i, L in enumerate(self.layers):
             v = variant % len(L.X)
-            dY = prev.dX if L.chained else L.dY[v]
             if hook is not None:
                 hook(i, L, False)
+            if L.attention is not None:
+                dY = self._attention_grad(L, prev, v)
+            elif L.loss is not None:
+                dY = self._loss_grad(L, v)
+            else:
+                dY = prev.dX if L.chained else L.dY[v]
             H = L.H[v % len(L.H)] if L.H is not None else None
             L.handle.dense_bwd(L.X[v], dY, L.W, H=H, dX=L.dX, dW=L.dW)
             if hook is not None:
@@ -120,7 +206,8 @@ class LinearStack:
 
     def probe(self, rho, nu, s: float, seed: int):
         """Alg. 1's probe for every layer (M = number of batch variants).  Returns a [L, 5] device tensor of
-        (V_s, V_act, V_w, p_lo, p_hi).  A chained layer is probed on its own gradient variants."""
+        (V_s, V_act, V_w, p_lo, p_hi).  A chained layer, or one under an attention
+        or a loss, is probed on its own gradient variants."""
         dev = self.layers[0].W.device
         out = torch.zeros(len(self.layers), 5, dtype=torch.float32, device=dev)
         for i, L in enumerate(self.layers):
