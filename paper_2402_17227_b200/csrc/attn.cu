@@ -393,9 +393,17 @@ cudaError_t bwd(const AttnCall& c, cudaStream_t st) {
 inline Attn* A(vcas_attn a) { return reinterpret_cast<Attn*>(a); }
 
 // Shared checks of a call's tensors; elements are addressed one by one, so that only the dtype's own alignment is asked for.
-bool good(const vcas_attn_tensor* x, int heads, int dim, size_t elem) {
+bool good(const vcas_attn_tensor* x, size_t elem) {
   return x != nullptr && x->ptr != nullptr && ((uintptr_t)x->ptr & (elem - 1)) == 0 && x->token >= 0 && x->head >= 0 &&
-         (heads == 1 || x->head >= dim) && x->token < (1ll << 40) && x->head < (1ll << 40);
+         x->token < (1ll << 40) && x->head < (1ll << 40);
+}
+// of one that is written, no two elements in one place
+bool good_out(const vcas_attn_tensor* x, int total, int heads, int dim, size_t elem) {
+  if (!good(x, elem)) return false;
+  const bool inner_head = x->head <= x->token;
+  const int64_t s0 = inner_head ? x->head : x->token, s1 = inner_head ? x->token : x->head;
+  const int64_t n0 = inner_head ? heads : total, n1 = inner_head ? total : heads;
+  return (n0 <= 1 || s0 >= dim) && (n1 <= 1 || s1 >= (n0 > 1 ? s0 * n0 : dim));
 }
 Strided S(const vcas_attn_tensor* x) { return Strided{x->ptr, x->token, x->head}; }
 
@@ -529,8 +537,7 @@ extern "C" int vcas_attn_fwd(vcas_attn aa, const vcas_attn_tensor* q, const vcas
   if (N == 0 || total == 0) return VCAS_OK;
   const size_t elem = a->desc.dtype == VCAS_DTYPE_BF16 ? 2 : 4;
   const int D = c.dim;
-  if (!good(q, c.heads_q, D, elem) || !good(k, c.heads_kv, D, elem) || !good(v, c.heads_kv, D, elem) ||
-      !good(o, c.heads_q, D, elem) || lse == nullptr)
+  if (!good(q, elem) || !good(k, elem) || !good(v, elem) || !good_out(o, total, c.heads_q, D, elem) || lse == nullptr)
     return VCAS_ERR_BAD_ARG;
   c.q = S(q); c.k = S(k); c.v = S(v); c.o = S(o); c.lse = lse;
   DeviceScope on(a->device);
@@ -552,9 +559,9 @@ extern "C" int vcas_attn_bwd(vcas_attn aa, const vcas_attn_tensor* d_o, const vc
   if (N == 0 || total == 0) return VCAS_OK;
   const size_t elem = a->desc.dtype == VCAS_DTYPE_BF16 ? 2 : 4;
   const int D = c.dim;
-  if (!good(q, c.heads_q, D, elem) || !good(k, c.heads_kv, D, elem) || !good(v, c.heads_kv, D, elem) || !good(o, c.heads_q, D, elem) ||
-      !good(d_o, c.heads_q, D, elem) || !good(dq, c.heads_q, D, elem) || !good(dk, c.heads_kv, D, elem) ||
-      !good(dv, c.heads_kv, D, elem) || lse == nullptr)
+  if (!good(q, elem) || !good(k, elem) || !good(v, elem) || !good(o, elem) || !good(d_o, elem) ||
+      !good_out(dq, total, c.heads_q, D, elem) || !good_out(dk, total, c.heads_kv, D, elem) ||
+      !good_out(dv, total, c.heads_kv, D, elem) || lse == nullptr)
     return VCAS_ERR_BAD_ARG;
   c.q = S(q); c.k = S(k); c.v = S(v); c.o = S(o); c.d_o = S(d_o); c.dq = S(dq); c.dk = S(dk); c.dv = S(dv);
   c.lse = const_cast<float*>(lse);

@@ -281,3 +281,80 @@ def test_refusals():
         op.fwd(big, big, big, packed([9]))
     with pytest.raises(vb.VcasError):
         op.fwd(x, x, x, packed([4, 4]))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("n", [33, 128, 129, 300])
+def test_sequences_of_every_length_in_any_number(dtype, causal, n):
+    """Tiles are taken in the order of their work while one warp can hold the lengths (128 of them), else as they come."""
+    g = torch.Generator().manual_seed(n)
+    lens = torch.randint(0, 40, (n,), generator=g).tolist()
+    lens[n // 2], lens[3], lens[n - 1] = 400, 260, 129
+    run(lens, 2, 1, 64, dtype, causal, "fused")
+    alive = sorted(torch.randperm(n, generator=g)[:n - 2].tolist())
+    run(lens, 2, 2, 64, dtype, causal, alive=alive)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_broadcast_inputs(dtype):
+    """Keys shared by all heads and values shared by all tokens as views with a stride of 0: read as such, gradients for each place."""
+    lens, H, D = [150, 33], 3, 64
+    T, starts = sum(lens), packed(lens)
+    q, k, v = tensors(T, H, H, D, dtype, "plain", 20)
+    do = tensors(T, H, H, D, dtype, "plain", 21)[0]
+    k, v = k[:, :1].expand(T, H, D), v[:1].expand(T, H, D)
+    op = vb.Attention(T, 2, H, H, D, dtype, causal=True)
+    ref = reference(q, k, v, starts, True, 0.125, do)
+    o, lse = op.fwd(q, k, v, starts)
+    check(o, ref["o"], what="o")
+    grads = op.bwd(do, q, k, v, ref["o"][0].to(dtype), ref["lse"][0].float(), starts)
+    for name, got in zip(("dq", "dk", "dv"), grads):
+        check(got, ref[name], what=name)
+    for out in (q[:1].expand(T, H, D), q[:, :1].expand(T, H, D)):
+        with pytest.raises(ValueError):
+            op.fwd(q, k, v, starts, o=out)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_two_handles_on_two_streams(D):
+    """Kernels of two handles in flight together share SMs and TMEM; each gives what it gives alone."""
+    lens = [700, 300, 129]
+    T, starts = sum(lens), packed(lens)
+    jobs = []
+    for i in range(2):
+        q, k, v = tensors(T, 8, 2, D, BF16, "fused", 30 + i)
+        do = tensors(T, 8, 2, D, BF16, "plain", 40 + i)[0]
+        op = vb.Attention(T, 3, 8, 2, D, BF16, causal=i == 0)
+        o, lse = op.fwd(q, k, v, starts)
+        alone = [x.clone() for x in (o, lse, *op.bwd(do, q, k, v, o, lse, starts))]
+        jobs.append((op, q, k, v, do, alone, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    got = [None, None]
+    for _ in range(10):
+        for i, (op, q, k, v, do, _, st) in enumerate(jobs):
+            with torch.cuda.stream(st):
+                o, lse = op.fwd(q, k, v, starts)
+                got[i] = (o, lse, *op.bwd(do, q, k, v, o, lse, starts))
+    torch.cuda.synchronize()
+    for i, (op, *_, alone, _) in enumerate(jobs):
+        assert op.device_status() == 0 and all(torch.equal(a, b) for a, b in zip(alone, got[i]))
+
+
+def test_score_range_that_a_first_tile_does_not_show():
+    """The first keys' scores far below the later ones (more than fp32's exponent away), and far above them."""
+    T, D = 400, 64
+    for sign in (1.0, -1.0):
+        g = torch.Generator("cuda").manual_seed(50)
+        q = torch.ones(T, 1, D, device="cuda")
+        k = 0.05 * torch.randn(T, 1, D, generator=g, device="cuda")
+        k += sign * 20.0 * (torch.arange(T, device="cuda")[:, None, None] >= 130).float()      # scores move by 160 / log 2 bits
+        v = torch.randn(T, 1, D, generator=g, device="cuda")
+        q, k, v = q.to(BF16), k.to(BF16), v.to(BF16)
+        starts = packed([T])
+        for causal in (False, True):
+            op = vb.Attention(T, 1, 1, 1, D, BF16, causal=causal)
+            ref = reference(q, k, v, starts, causal, 0.125)
+            o, lse = op.fwd(q, k, v, starts)
+            check(o, ref["o"], what="o")
+            check(lse, ref["lse"], what="lse")
