@@ -70,6 +70,17 @@ __device__ __forceinline__ void product_tiles(uint32_t d, uint32_t a, uint32_t b
     for (int k = 0; k < 4; ++k) umma_bf16(d, da + (uint64_t)(k * 2), db + (uint64_t)(k * 2), idesc, (c | k) != 0 ? 1u : 0u);
   }
 }
+// the same with A in TMEM, 32 DC columns of bf16 pairs
+template <int DC, int TN>
+__device__ __forceinline__ void product_tiles_ts(uint32_t d, uint32_t a, uint32_t b) {
+  constexpr uint32_t idesc = make_idesc(TN, false, false);
+#pragma unroll
+  for (int c = 0; c < DC; ++c) {
+    const uint64_t db = desc_kmajor(b + c * CHUNK<TN>);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) umma_bf16_ts(d, a + (uint32_t)(c * 32 + k * 8), db + (uint64_t)(k * 2), idesc, (c | k) != 0 ? 1u : 0u);
+  }
+}
 // D [128 x 64 DC] (+)= A B, A [128 x TN] bf16 in TMEM (each 64 of its columns `gap` TMEM columns behind the 64 before), B a tile of
 // TN rows
 template <int DC, int TN, int K0, int K1>           // columns 16 K0 .. 16 K1 of A
@@ -92,18 +103,25 @@ __device__ __forceinline__ void load_tile(uint8_t* dst, const CUtensorMap* map, 
 #pragma unroll
   for (int c = 0; c < DC; ++c) tma_load_3d(dst + c * CHUNK<ROWS>, map, 64 * c, head, token, bar);
 }
-// sum over 64 columns of a row of two tiles of their products
-__device__ __forceinline__ float row_dot(const uint8_t* a, const uint8_t* b, int row) {
+// 64 columns of a row of a tile of 128 rows, as 32 pairs
+__device__ __forceinline__ void read_row(const uint8_t* tile, int row, uint32_t (&v)[32]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint4 x = *reinterpret_cast<const uint4*>(tile + row * 128 + ((i ^ (row & 7)) << 4));        // the 128-byte swizzle
+    v[4 * i] = x.x; v[4 * i + 1] = x.y; v[4 * i + 2] = x.z; v[4 * i + 3] = x.w;
+  }
+}
+// the sum of its products with v
+__device__ __forceinline__ float row_dot(const uint8_t* tile, int row, const uint32_t (&v)[32]) {
   float s0 = 0.f, s1 = 0.f;
-#pragma unroll 2
-  for (int v = 0; v < 8; ++v) {
-    const int at = row * 128 + ((v ^ (row & 7)) << 4);           // the 128-byte swizzle
-    const uint4 x = *reinterpret_cast<const uint4*>(a + at), y = *reinterpret_cast<const uint4*>(b + at);
-    const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint4 x = *reinterpret_cast<const uint4*>(tile + row * 128 + ((i ^ (row & 7)) << 4));
+    const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      s0 = fmaf(__uint_as_float(xs[e] << 16), __uint_as_float(ys[e] << 16), s0);
-      s1 = fmaf(__uint_as_float(xs[e] & 0xffff0000u), __uint_as_float(ys[e] & 0xffff0000u), s1);
+      s0 = fmaf(__uint_as_float(xs[e] << 16), __uint_as_float(v[4 * i + e] << 16), s0);
+      s1 = fmaf(__uint_as_float(xs[e] & 0xffff0000u), __uint_as_float(v[4 * i + e] & 0xffff0000u), s1);
     }
   }
   return s0 + s1;
@@ -159,7 +177,7 @@ struct Shared {
   uint64_t scores[2], dscores;                       // products of which the scores' warps wait
   uint64_t ready[2];                                 // P, dS written
   uint64_t done, acc_empty;                          // accumulators complete, and read
-  uint64_t o_read, drain;
+  uint64_t taken, drain;                             // dQ: the own tiles have been read
   uint64_t added;                                    // forward: P V of a tile is in O
   uint64_t rows_full[2][2];                          // dK, dV: the queries' values, by column half and buffer
   uint32_t tmem;
@@ -207,7 +225,7 @@ __device__ __forceinline__ void begin(Shared& s, const UmmaCall& P, int stages, 
     mbar_init(&s.dscores, 1);
     mbar_init(&s.done, 1);
     mbar_init(&s.acc_empty, warps);
-    mbar_init(&s.o_read, warps);
+    mbar_init(&s.taken, warps);
     mbar_init(&s.added, 1);
     for (int i = 0; i < 4; ++i) mbar_init(&s.rows_full[i >> 1][i & 1], 4);
     mbar_init(&s.drain, 1);
@@ -519,8 +537,10 @@ template <int DC> constexpr int BWD_THREADS = 32 * (BWD_WARPS<DC> + 2);
 template <int DC> constexpr int BWD_CTAS = DC == 1 ? 2 : 1;
 template <int DC> constexpr int BWD_STAGES = DC == 1 ? 6 : 5;
 
-// Rows are queries.  TMEM: two score tiles in turn (dS replaces its own), dP, dQ.  O comes once, for delta = rowsum(dO O): in the ring
-// where its tiles are as large (DC = 2), else beside Q and dO.
+// Rows are queries.  TMEM: S, dP (dS replaces it), dQ, and Q and dO as A operands of all products with them: read from shared memory for
+// each tile, with both operands there, they took most of its bandwidth (a tile of 128 keys 2290 cycles; with them and S in place of
+// a second S, NOW_TILE).  S is free for the next tile's scores as soon as the warps have read it.  O comes once a tile of rows, for
+// delta = rowsum(dO O): in the ring where its tiles are as large (DC = 2), else beside Q and dO.
 template <int DC>
 __global__ void __launch_bounds__(BWD_THREADS<DC>, BWD_CTAS<DC>)
 attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mdo, const __grid_constant__ CUtensorMap mo,
@@ -528,6 +548,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
   constexpr int STAGES = BWD_STAGES<DC>, TN = TN_OF<DC>, WARPS = BWD_WARPS<DC>, OWN = DC * CHUNK<128>, TILE = DC * CHUNK<TN>;
   constexpr bool O_IN_RING = DC == 2;
   static_assert(!O_IN_RING || TN == 128, "as large as a tile of the ring");
+  static_assert(WARPS == 4 * DC, "every 64 columns have a warp");
   extern __shared__ __align__(1024) uint8_t smem[];
   uint8_t *sq = smem, *sdo = sq + OWN, *so = sdo + OWN, *ring = O_IN_RING ? so : so + OWN;
   float* s_half = reinterpret_cast<float*>(ring + STAGES * TILE);    // [DC][128] parts of delta
@@ -539,9 +560,10 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
   // all before it is done); the wait at the end makes sure that this one does not end first.  The dK, dV kernel's CTAs may come as
   // soon as the last ones of this grid have begun.
   pdl_trigger();
-  begin(s, P, STAGES, WARPS, WARPS, 4 * TN);
+  begin(s, P, STAGES, WARPS, WARPS - 1, 4 * TN);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t ts = s.tmem, tdp = ts + 2 * TN, tdq = ts + 3 * TN;
+  const uint32_t ts = s.tmem, tdp = ts + TN, tdq = ts + 2 * TN, tq = tdq + 64 * DC, tdo = tq + 32 * DC;
+  static_assert(2 * TN + 128 * DC == 4 * TN, "all columns");
   volatile int* ab = &s.abort_flag;
   int32_t* status = C.seqs.status;
   auto tiles_of = [&](const Item& it) { return ((C.causal ? min(it.len, it.t0 + 128) : it.len) + TN - 1) / TN; };
@@ -571,11 +593,9 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
       ++own;
       const int tiles = tiles_of(it), kv = it.head / C.group;
       const bool stall = P.stall_once && blockIdx.x == 0 && n == 0;
-      for (int i = 0; i < 2 * tiles && ok; ++i) {
+      if (O_IN_RING) ok = fill<DC, TN>(s, r, STAGES, ring, &mo, it.head, token, false, status);
+      for (int i = 0; i < 2 * tiles && ok; ++i)
         ok = fill<DC, TN>(s, r, STAGES, ring, (i & 1) ? &mv : &mk, kv, it.first + (i >> 1) * TN, stall && i == 0, status);
-        // behind the first two tiles, which the first products need
-        if (O_IN_RING && i == 1) ok = ok && fill<DC, TN>(s, r, STAGES, ring, &mo, it.head, token, false, status);
-      }
       if (!ok) break;
     }
     if (lane == 0) drain(s, r, STAGES, own, status);
@@ -583,13 +603,18 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
     const bool leader = elect_one();
     Ring r;
     Item it;
-    uint32_t made = 0;                   // dS tiles so far
-    int score = 0;                       // score tiles so far
+    uint32_t made = 0;                   // tiles of scores so far
     bool ok = true;
     for (int n = 0; ok && get_item(s, n, status, it); ++n) {
       const int tiles = tiles_of(it);
-      ok = warp_wait(&s.own_full, n & 1, ab, status);
+      // Q and dO are in TMEM, and O has been read
+      ok = warp_wait(&s.taken, n & 1, ab, status);
       if (!ok) break;
+      tc_fence_after();
+      if (O_IN_RING) {
+        if (leader) mbar_arrive(&s.empty[r.stage]);
+        r.next(STAGES);
+      }
       int k_now = 0, k_next = 0;         // ring places of this tile's K and the next one's
       // waits for the next tile of the ring; rows behind the sequence's end become 0
       auto arrived = [&](int j) {
@@ -608,34 +633,28 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         k_next = arrived(j);
         if (!ok) return;
         if (leader) {
-          product_tiles<DC, TN>(ts + (score & 1) * TN, smem_u32(sq), smem_u32(ring + k_next * TILE));
-          umma_commit(&s.scores[score & 1]);
+          product_tiles_ts<DC, TN>(ts, tq, smem_u32(ring + k_next * TILE));
+          umma_commit(&s.scores[0]);
         }
-        ++score;
       };
       auto dscores = [&](int j) {
         const int v = arrived(j);
         if (!ok) return;
         if (leader) {
-          product_tiles<DC, TN>(tdp, smem_u32(sdo), smem_u32(ring + v * TILE));
+          product_tiles_ts<DC, TN>(tdp, tdo, smem_u32(ring + v * TILE));
           umma_commit(&s.dscores);
           umma_commit(&s.empty[v]);
-          if (j == tiles - 1) umma_commit(&s.own_empty);
         }
       };
       scores(0);
       if (!ok) break;
       dscores(0);
       if (!ok) break;
-      if (O_IN_RING) {
-        // O's place is given back when the other warps have read it
-        ok = warp_wait(&s.o_read, n & 1, ab, status);
-        if (!ok) break;
-        if (leader) mbar_arrive(&s.empty[r.stage]);
-        r.next(STAGES);
-      }
       for (int j = 0; j < tiles; ++j, ++made) {
         k_now = k_next;
+        ok = warp_wait(&s.ready[1], made & 1, ab, status);       // S has been read
+        if (!ok) break;
+        tc_fence_after();
         if (j + 1 < tiles) {
           scores(j + 1);
           if (!ok) break;
@@ -644,63 +663,70 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         ok = ok && warp_wait(&s.ready[0], made & 1, ab, status);
         if (!ok) break;
         tc_fence_after();
-        if (j + 1 < tiles) dscores(j + 1);
-        if (!ok) break;
         if (leader) {
-          product_rows<DC, TN, 0, TN / 16>(tdq, ts + (made & 1) * TN, 64, smem_u32(ring + k_now * TILE), j != 0);
+          product_rows<DC, TN, 0, TN / 16>(tdq, tdp, 64, smem_u32(ring + k_now * TILE), j != 0);
           umma_commit(&s.empty[k_now]);
           if (j == tiles - 1) umma_commit(&s.done);
         }
+        if (j + 1 < tiles) dscores(j + 1);
+        if (!ok) break;
       }
     }
     if (leader && *ab) drain_products(&s.drain, ab, status);
   } else {
-    const int part = warp >> 2;          // columns part * 64 ..
+    const int part = warp >> 2, in = (warp & 3) * 32 + lane;     // columns part * 64 ..; row of the tile
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const float c = C.scale * ATTN_LOG2E;
     const uint64_t c2 = pack2(c, c);
-    Item it;
+    Item it, prev;
+    float lse = 0.f, delta = 0.f;
     uint32_t made = 0;
     Ring r;                              // the loads, to find O among them
     bool ok = true;
-    float lse = 0.f;
-    const int in = (warp & 3) * 32 + lane;
-    for (int n = 0; ok && get_item(s, n, status, it, s_lse + in, &lse); ++n) {
-      const int tiles = tiles_of(it), row = it.t0 + in;
-      const int64_t at_row = (int64_t)it.head * C.seqs.total + it.first + row;
+    // the next tile of rows: Q and dO to TMEM, delta (which the dK, dV kernel reads)
+    auto take = [&](int n) -> bool {
+      if (!get_item(s, n, status, it, s_lse + in, &lse)) return false;
       ok = warp_wait(&s.own_full, n & 1, ab, status);
-      if (!ok) break;
+      if (!ok) return false;
+      uint32_t v[32];
+      read_row(sq + part * CHUNK<128>, in, v);
+      tmem_st32(tq + lanes + part * 32, v);
+      read_row(sdo + part * CHUNK<128>, in, v);
+      tmem_st32(tdo + lanes + part * 32, v);
       const uint8_t* o_tile = so;
       if (O_IN_RING) {
-        r.next(STAGES);
-        r.next(STAGES);
         ok = warp_wait(&s.full[r.stage], r.phase, ab, status);
-        if (!ok) break;
+        if (!ok) return false;
         o_tile = ring + r.stage * TILE;
-        r.next(STAGES);
-        for (int i = 2; i < 2 * tiles; ++i) r.next(STAGES);
+        for (int i = 0; i < 1 + 2 * tiles_of(it); ++i) r.next(STAGES);
       }
-      // a warp sums over 64 columns; the dK, dV kernel reads delta
-      static_assert(WARPS == 4 * DC, "every 64 columns have a warp");
-      float delta = row_dot(sdo + part * CHUNK<128>, o_tile + part * CHUNK<128>, in);
+      delta = row_dot(o_tile + part * CHUNK<128>, in, v);
       if (DC == 2) s_half[part * 128 + in] = delta;
-      warp_arrive(&s.o_read);
+      tmem_wait_st();
+      tc_fence_before();
+      warp_arrive(&s.taken);
       warp_arrive(&s.own_empty);
+      return true;
+    };
+    bool more = take(0);
+    for (int n = 0; more; ++n) {
+      const int tiles = tiles_of(it), row = it.t0 + in;
       if (DC == 2) {
-        ok = warp_wait(&s.o_read, n & 1, ab, status);
+        ok = warp_wait(&s.taken, n & 1, ab, status);
         if (!ok) break;
         delta = s_half[in] + s_half[128 + in];
       }
-      if (part == 0 && row < it.len) C.delta[at_row] = delta;
+      if (part == 0 && row < it.len) C.delta[(int64_t)it.head * C.seqs.total + it.first + row] = delta;
       const float nl = -lse * ATTN_LOG2E;
       const uint64_t n2 = pack2(nl, nl), d2 = pack2(-delta, -delta);
       for (int j = 0; j < tiles; ++j, ++made) {
-        ok = warp_wait(&s.scores[made & 1], (made >> 1) & 1, ab, status);
+        ok = warp_wait(&s.scores[0], made & 1, ab, status);
         if (!ok) break;
         tc_fence_after();
-        const uint32_t at = ts + lanes + (made & 1) * TN + part * 64;
         uint32_t a[64];
-        tmem_ld64(at, a);
+        tmem_ld64(ts + lanes + part * 64, a);
+        tc_fence_before();
+        warp_arrive(&s.ready[1]);
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
           float e0, e1;
@@ -728,19 +754,22 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             o[i] = pack_bf16(s0, s1);
           }
         }
-        tmem_st32(at, o);
+        tmem_st32(tdp + lanes + part * 64, o);
         tmem_wait_st();
         tc_fence_before();
         warp_arrive(&s.ready[0]);
       }
       ok = ok && warp_wait(&s.done, n & 1, ab, status);
       if (!ok) break;
-      // a warp stores 64 columns
       tc_fence_after();
+      // the next tile's first products run while this one's rows are stored, 64 columns by a warp
+      prev = it;
+      more = take(n + 1);
+      if (!ok) break;
       Strided x = C.dq;
       x.p = (const __nv_bfloat16*)x.p + part * 64;
-      const int warp_row = it.t0 + (warp & 3) * 32;
-      store_rows<1>(tdq + lanes + part * 64, x, (int64_t)it.first + warp_row, it.head, C.dim - part * 64, it.len - warp_row, C.scale);
+      const int warp_row = prev.t0 + (warp & 3) * 32;
+      store_rows<1>(tdq + lanes + part * 64, x, (int64_t)prev.first + warp_row, prev.head, C.dim - part * 64, prev.len - warp_row, C.scale);
       tc_fence_before();
       warp_arrive(&s.acc_empty);
     }
