@@ -260,6 +260,12 @@ struct Ring {
   __device__ __forceinline__ void next(int stages) {
     if (++stage == stages) { stage = 0; phase ^= 1u; }
   }
+  template <int STAGES>
+  __device__ __forceinline__ void skip(int n) {
+    stage += n;
+    phase ^= (uint32_t)(stage / STAGES) & 1u;
+    stage %= STAGES;
+  }
 };
 // The loading warp's part: takes the next tile off the counter and tells the others.  The counter goes through the heads first, so that
 // CTAs at work at the same time share the other side's tiles, then through the tiles in the order of `Order`.
@@ -538,8 +544,8 @@ template <int DC> constexpr int BWD_CTAS = DC == 1 ? 2 : 1;
 template <int DC> constexpr int BWD_STAGES = DC == 1 ? 6 : 5;
 
 // Rows are queries.  TMEM: S, dP (dS replaces it), dQ, and Q and dO as A operands of all products with them: read from shared memory for
-// each tile, with both operands there, they took most of its bandwidth (a tile of 128 keys 2290 cycles; with them and S in place of
-// a second S, NOW_TILE).  S is free for the next tile's scores as soon as the warps have read it.  O comes once a tile of rows, for
+// each tile, with both operands there, they took most of its bandwidth (a tile of 128 keys 2290 cycles; with them in TMEM, and one S in
+// place of two, 2140).  S is free for the next tile's scores as soon as the warps have read it.  O comes once a tile of rows, for
 // delta = rowsum(dO O): in the ring where its tiles are as large (DC = 2), else beside Q and dO.
 template <int DC>
 __global__ void __launch_bounds__(BWD_THREADS<DC>, BWD_CTAS<DC>)
@@ -580,23 +586,33 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
       prefetch_map(&mk);
       prefetch_map(&mv);
     }
-    for (int n = 0; take_item(s, P, order, n, C.heads_q, it, s_lse); ++n) {
-      bool ok = warp_wait(&s.own_empty, (n & 1) ^ 1, ab, status);
-      if (!ok) break;
-      const int token = it.first + it.t0;
+    // Q, dO (and O) of a tile of rows: their place is free as soon as those of the one before have been taken
+    auto load_own = [&](int n, const Item& x) -> bool {
+      if (!warp_wait(&s.own_empty, (n & 1) ^ 1, ab, status)) return false;
       if (elect_one()) {
         mbar_expect_tx(&s.own_full, (O_IN_RING ? 2 : 3) * OWN);
-        load_tile<DC, 128>(sq, &mq, it.head, token, &s.own_full);
-        load_tile<DC, 128>(sdo, &mdo, it.head, token, &s.own_full);
-        if (!O_IN_RING) load_tile<DC, 128>(so, &mo, it.head, token, &s.own_full);
+        load_tile<DC, 128>(sq, &mq, x.head, x.first + x.t0, &s.own_full);
+        load_tile<DC, 128>(sdo, &mdo, x.head, x.first + x.t0, &s.own_full);
+        if (!O_IN_RING) load_tile<DC, 128>(so, &mo, x.head, x.first + x.t0, &s.own_full);
       }
       ++own;
-      const int tiles = tiles_of(it), kv = it.head / C.group;
+      return true;
+    };
+    bool more = take_item(s, P, order, 0, C.heads_q, it, s_lse), ok = !more || load_own(0, it);
+    for (int n = 0; more && ok; ++n) {
+      Item next = it;
+      const int tiles = tiles_of(it), kv = it.head / C.group, from = O_IN_RING ? -1 : 0, loads = 2 * tiles - from;
       const bool stall = P.stall_once && blockIdx.x == 0 && n == 0;
-      if (O_IN_RING) ok = fill<DC, TN>(s, r, STAGES, ring, &mo, it.head, token, false, status);
-      for (int i = 0; i < 2 * tiles && ok; ++i)
-        ok = fill<DC, TN>(s, r, STAGES, ring, (i & 1) ? &mv : &mk, kv, it.first + (i >> 1) * TN, stall && i == 0, status);
-      if (!ok) break;
+      for (int i = from; i < 2 * tiles && ok; ++i) {
+        if (i < 0) ok = fill<DC, TN>(s, r, STAGES, ring, &mo, it.head, it.first + it.t0, false, status);
+        else ok = fill<DC, TN>(s, r, STAGES, ring, (i & 1) ? &mv : &mk, kv, it.first + (i >> 1) * TN, stall && i == 0, status);
+        if (ok && i - from == min(loads, STAGES) - 1) {
+          // the ring is full or this tile's loads are on their way: time to see to the next one
+          more = take_item(s, P, order, n + 1, C.heads_q, next, s_lse);
+          if (more) ok = load_own(n + 1, next);
+        }
+      }
+      it = next;
     }
     if (lane == 0) drain(s, r, STAGES, own, status);
   } else if (warp == WARPS) {
@@ -698,7 +714,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         ok = warp_wait(&s.full[r.stage], r.phase, ab, status);
         if (!ok) return false;
         o_tile = ring + r.stage * TILE;
-        for (int i = 0; i < 1 + 2 * tiles_of(it); ++i) r.next(STAGES);
+        r.skip<STAGES>(1 + 2 * tiles_of(it));
       }
       delta = row_dot(o_tile + part * CHUNK<128>, in, v);
       if (DC == 2) s_half[part * 128 + in] = delta;
