@@ -168,17 +168,17 @@ __device__ __forceinline__ void store_rows(uint32_t taddr, const Strided& x, int
 }
 
 // ----------------------------------------------------------------------------------------- the CTA
-constexpr int MAX_STAGES = 8;
+constexpr int MAX_STAGES = 10;
 struct Item { int first, len, t0, head, any; };      // a tile of 128 rows: its sequence, its first row in there, its head
 struct Shared {
   uint64_t full[MAX_STAGES], empty[MAX_STAGES];      // ring of the other side's tiles
   uint64_t item_full[2], item_empty[2];
   uint64_t own_full, own_empty;                      // the item's own tiles
-  uint64_t scores[2], dscores;                       // products of which the scores' warps wait
-  uint64_t ready[2];                                 // P, dS written
-  uint64_t done, acc_empty;                          // accumulators complete, and read
-  uint64_t taken, drain;                             // dQ: the own tiles have been read
-  uint64_t added;                                    // forward: P V of a tile is in O
+  uint64_t scores[4], dscores;                       // products of which the scores' warps wait
+  uint64_t ready[4];                                 // P, dS written
+  uint64_t done[2], acc_empty[2];                    // accumulators complete, and read
+  uint64_t taken, drain[2];                          // dQ: the own tiles have been read
+  uint64_t added[2];                                 // forward: P V of a tile is in O
   uint64_t rows_full[2][2];                          // dK, dV: the queries' values, by column half and buffer
   uint32_t tmem;
   int abort_flag;                                    // mbar_wait finds the limit 20 bytes behind it
@@ -210,25 +210,27 @@ __device__ __forceinline__ bool in_place(const uint8_t* smem, int32_t* status) {
   if (threadIdx.x == 0) atomicExch(status, (int32_t)VCAS_ERR_INTERNAL);
   return false;
 }
-// Sets the barriers up and takes TMEM.  warps: those that work on scores.
-__device__ __forceinline__ void begin(Shared& s, const UmmaCall& P, int stages, uint32_t warps, uint32_t own_readers, uint32_t columns) {
+// Sets the barriers up and takes TMEM.  warps: those that work on scores, `team` of them on the same ones.
+// issuers: warps that issue products; own_arrivals: with which the own tiles are given back.
+__device__ __forceinline__ void begin(Shared& s, const UmmaCall& P, int stages, uint32_t warps, uint32_t team, uint32_t issuers,
+                                      uint32_t own_arrivals, uint32_t columns) {
   if (threadIdx.x == 0) {
-    for (int i = 0; i < stages; ++i) { mbar_init(&s.full[i], 1); mbar_init(&s.empty[i], 1); }
+    for (int i = 0; i < stages; ++i) { mbar_init(&s.full[i], 1); mbar_init(&s.empty[i], issuers); }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&s.item_full[i], 1);
-      mbar_init(&s.item_empty[i], warps + 1);
-      mbar_init(&s.scores[i], 1);
-      mbar_init(&s.ready[i], warps);
+      mbar_init(&s.item_empty[i], warps + issuers);
+      mbar_init(&s.done[i], 1);
+      mbar_init(&s.acc_empty[i], team);
+      mbar_init(&s.added[i], 1);
     }
+    for (int i = 0; i < 4; ++i) { mbar_init(&s.scores[i], 1); mbar_init(&s.ready[i], team); }
     mbar_init(&s.own_full, 1);
-    mbar_init(&s.own_empty, 1 + own_readers);
+    mbar_init(&s.own_empty, own_arrivals);
     mbar_init(&s.dscores, 1);
-    mbar_init(&s.done, 1);
-    mbar_init(&s.acc_empty, warps);
     mbar_init(&s.taken, warps);
-    mbar_init(&s.added, 1);
     for (int i = 0; i < 4; ++i) mbar_init(&s.rows_full[i >> 1][i & 1], 4);
-    mbar_init(&s.drain, 1);
+    mbar_init(&s.drain[0], 1);
+    mbar_init(&s.drain[1], 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     s.abort_flag = 0;
     s.limit = P.wait_limit_ns;
@@ -325,34 +327,39 @@ __device__ __forceinline__ void drain(Shared& s, const Ring& r, int stages, uint
 }
 
 // ------------------------------------------------------------------------------------------ forward
-// Two CTAs an SM, each with 128 query rows, against tiles of 64 keys: two of them in TMEM (64 columns each, beside O's 64 DC), so that a
-// tile's scores are there when the warps come from the one before, and the products of two CTAs fill the tensor pipe.  (8 x 2048 tokens,
-// 32/8 heads of 128, causal: 273 us; key tiles of 128, one at a time, 292: 1506 of a tile's 3644 cycles went by between the last P and the
-// next scores.)  What bounds it: 64-wide products with A in shared memory take 427 cycles for 256 of arithmetic, so that the tensor pipe is
-// busy 78 % of the time; the exponentials take 58 % of theirs.  (A part of them as polynomials on the FMA pipe: 298 us for one in eight of
-// the pairs, 303 for two; the warps' issue slots were what it cost.)
+// 128 query rows of one head (two CTAs an SM) or of two heads that share keys and values (one), against tiles of 64 keys: two tiles of
+// scores of each head are in TMEM (64 columns each, beside O's 64 DC), so that a tile's scores are there when the warps come from the
+// one before, and the products of two heads or CTAs fill the tensor pipe.  (Key tiles of 128, one at a time: 1506 of a tile's 3644 cycles
+// went by between the last P and the next scores.)
+// Bound by shared memory: Q is read for each tile of keys (there is no room for it in TMEM), 64-wide products with both operands there
+// take 427 cycles for 256 of arithmetic, and the tiles have to be written too.  Two heads on one copy of K and V save a sixth of
+// that: for heads wider than 64 in groups of an even number (8 x 2048 tokens, 32/8 heads of 128, causal: 282 us by one head, 267
+// by two); narrower ones are bound by their exponentials.  (A part of these as polynomials on the FMA pipe: 298 us for one in eight of
+// the pairs where all by the special function unit took 292; the warps' issue slots were what it cost.)
 constexpr int FWD_TN = 64;
-template <int DC> constexpr int FWD_STAGES = DC == 1 ? 8 : 5;
-constexpr int FWD_THREADS = 192;
+template <int DC, int HEADS> constexpr int FWD_STAGES = HEADS == 2 ? 10 : DC == 1 ? 8 : 5;
+template <int HEADS> constexpr int FWD_THREADS = 160 * HEADS + 32;
 
-template <int DC>
-__global__ void __launch_bounds__(FWD_THREADS, 2)
+template <int DC, int HEADS>
+__global__ void __launch_bounds__(FWD_THREADS<HEADS>, HEADS == 2 ? 1 : 2)
 attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                 const __grid_constant__ UmmaCall P) {
-  constexpr int STAGES = FWD_STAGES<DC>, TN = FWD_TN, OWN = DC * CHUNK<128>, TILE = DC * CHUNK<TN>;
+  constexpr int STAGES = FWD_STAGES<DC, HEADS>, TN = FWD_TN, OWN = DC * CHUNK<128>, TILE = DC * CHUNK<TN>, COLUMNS = 256 * HEADS;
   extern __shared__ __align__(1024) uint8_t smem[];
-  uint8_t *sq = smem, *ring = smem + OWN;
+  uint8_t *sq = smem, *ring = smem + HEADS * OWN;
   Shared& s = *reinterpret_cast<Shared*>(ring + STAGES * TILE);
   const AttnCall& C = P.c;
   if (!in_place(smem, C.seqs.status)) return;
-  begin(s, P, STAGES, 4, 0, 256);
+  begin(s, P, STAGES, 4 * HEADS, 4, HEADS, HEADS, COLUMNS);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t ts = s.tmem, to = s.tmem + 2 * TN;
+  // TMEM of head h: two tiles of scores, O
+  auto scores_of = [&](int h) { return s.tmem + (uint32_t)(h * 256); };
+  auto out_of = [&](int h) { return s.tmem + (uint32_t)(h * 256 + 2 * TN); };
   volatile int* ab = &s.abort_flag;
   int32_t* status = C.seqs.status;
   auto tiles_of = [&](const Item& it) { return ((C.causal ? min(it.len, it.t0 + 128) : it.len) + TN - 1) / TN; };
 
-  if (warp == 5) {
+  if (warp == 5 * HEADS) {
     const Order order(C.seqs, lane, C.causal, false);
     Ring r;
     Item it;
@@ -362,15 +369,16 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
       prefetch_map(&mk);
       prefetch_map(&mv);
     }
-    for (int n = 0; take_item(s, P, order, n, C.heads_q, it); ++n) {
+    for (int n = 0; take_item(s, P, order, n, C.heads_q / HEADS, it); ++n) {
       bool ok = warp_wait(&s.own_empty, (n & 1) ^ 1, ab, status);
       if (!ok) break;
       if (elect_one()) {
-        mbar_expect_tx(&s.own_full, OWN);
-        load_tile<DC, 128>(sq, &mq, it.head, it.first + it.t0, &s.own_full);
+        mbar_expect_tx(&s.own_full, HEADS * OWN);
+#pragma unroll
+        for (int h = 0; h < HEADS; ++h) load_tile<DC, 128>(sq + h * OWN, &mq, it.head * HEADS + h, it.first + it.t0, &s.own_full);
       }
       ++own;
-      const int tiles = tiles_of(it), kv = it.head / C.group;
+      const int tiles = tiles_of(it), kv = it.head * HEADS / C.group;
       const bool stall = P.stall_once && blockIdx.x == 0 && n == 0;
       // in the order of their use: K 0, K 1, V 0, K 2, V 1, ...
       for (int j = 0; j <= tiles && ok; ++j) {
@@ -380,7 +388,10 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
       if (!ok) break;
     }
     if (lane == 0) drain(s, r, STAGES, own, status);
-  } else if (warp == 4) {
+  } else if (warp >= 4 * HEADS) {
+    // one for each head: a head's products do not wait for the other's probabilities
+    const int h = warp - 4 * HEADS;
+    const uint32_t ts = scores_of(h), to = out_of(h), q = smem_u32(sq + h * OWN);
     const bool leader = elect_one();
     Ring r;
     Item it;
@@ -395,9 +406,9 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         if (!ok) return;
         tc_fence_after();
         if (leader) {
-          product_tiles<DC, TN>(ts + (score & 1) * TN, smem_u32(sq), smem_u32(ring + r.stage * TILE));
+          product_tiles<DC, TN>(ts + (score & 1) * TN, q, smem_u32(ring + r.stage * TILE));
           umma_commit(&s.empty[r.stage]);
-          umma_commit(&s.scores[score & 1]);
+          umma_commit(&s.scores[2 * h + (score & 1)]);
           if (last) umma_commit(&s.own_empty);
         }
         ++score;
@@ -409,42 +420,43 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         ok = warp_wait(&s.full[r.stage], r.phase, ab, status);
         if (!ok) break;
         const int have = it.len - j * TN, place = r.stage;
-        if (have < TN) {
+        if (have < TN) {                 // zeros over zeros where the other head's warp has been
           zero_rows<DC, TN>(ring + place * TILE, have, lane);
           fence_async_smem();
           __syncwarp();
         }
         r.next(STAGES);
-        if (j == 0) ok = warp_wait(&s.acc_empty, (n & 1) ^ 1, ab, status);
-        ok = ok && warp_wait(&s.ready[made & 1], (made >> 1) & 1, ab, status);
+        if (j == 0) ok = warp_wait(&s.acc_empty[h], (n & 1) ^ 1, ab, status);
+        ok = ok && warp_wait(&s.ready[2 * h + (made & 1)], (made >> 1) & 1, ab, status);
         if (!ok) break;
         tc_fence_after();
         if (leader) {
           product_rows<DC, TN, 0, TN / 16>(to, ts + (made & 1) * TN, 0, smem_u32(ring + place * TILE), j != 0);
           umma_commit(&s.empty[place]);
-          umma_commit(&s.added);
-          if (j == tiles - 1) umma_commit(&s.done);
+          umma_commit(&s.added[h]);
+          if (j == tiles - 1) umma_commit(&s.done[h]);
         }
         if (j + 2 < tiles) scores(j + 3 == tiles);
       }
     }
-    if (leader && *ab) drain_products(&s.drain, ab, status);
+    if (leader && *ab) drain_products(&s.drain[h], ab, status);
   } else {
-    const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+    const int h = warp >> 2, in = threadIdx.x & 127;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, ts = scores_of(h), to = out_of(h);
     const float c = C.scale * ATTN_LOG2E, none = __int_as_float(0xff800000);
     const uint64_t c2 = pack2(c, c);
     Item it;
     uint32_t made = 0;
     bool ok = true;
     for (int n = 0; ok && get_item(s, n, status, it); ++n) {
-      const int row = it.t0 + threadIdx.x, tiles = tiles_of(it);         // row: in the sequence
+      const int row = it.t0 + in, tiles = tiles_of(it), head = it.head * HEADS + h;      // row: in the sequence
       // Sums are relative to 2^m, m near the largest score so far (times c).  They are floats, so it need not be the largest:
       // exponentials are taken before the tile's own maximum is known (with it first, 395 cycles per 128 keys went by without an
       // exponential on its way), m follows once the maximum is 8 above it, and at once where 2^64 is passed.
       float m = 0.f, l = 0.f, over = 0.f;            // over: the last tile's maximum above m
       auto lift = [&](float by, bool mine) {
         // O must be complete up to the tile before this one
-        ok = warp_wait(&s.added, (made - 1) & 1, ab, status);
+        ok = warp_wait(&s.added[h], (made - 1) & 1, ab, status);
         if (!ok) return;
         tc_fence_after();
         const float f = mine ? attn_exp2(-by) : 1.0f;
@@ -461,7 +473,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         tmem_wait_st();
       };
       for (int j = 0; j < tiles; ++j, ++made) {
-        ok = warp_wait(&s.scores[made & 1], (made >> 1) & 1, ab, status);
+        ok = warp_wait(&s.scores[2 * h + (made & 1)], (made >> 1) & 1, ab, status);
         if (!ok) break;
         tc_fence_after();
         const uint32_t at = ts + lanes + (made & 1) * TN;
@@ -518,18 +530,19 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         tmem_st32(at, o);
         tmem_wait_st();
         tc_fence_before();
-        warp_arrive(&s.ready[made & 1]);
+        warp_arrive(&s.ready[2 * h + (made & 1)]);
       }
-      ok = ok && warp_wait(&s.done, n & 1, ab, status);
+      ok = ok && warp_wait(&s.done[h], n & 1, ab, status);
       if (!ok) break;
       tc_fence_after();
-      store_rows<DC>(to + lanes, C.o, (int64_t)it.first + it.t0 + warp * 32, it.head, C.dim, it.len - it.t0 - warp * 32, 1.0f / l);
+      const int warp_row = it.t0 + (warp & 3) * 32;
+      store_rows<DC>(to + lanes, C.o, (int64_t)it.first + warp_row, head, C.dim, it.len - warp_row, 1.0f / l);
       tc_fence_before();
-      warp_arrive(&s.acc_empty);
-      if (row < it.len) C.lse[(int64_t)it.head * C.seqs.total + it.first + row] = m * ATTN_LN2 + logf(l);
+      warp_arrive(&s.acc_empty[h]);
+      if (row < it.len) C.lse[(int64_t)head * C.seqs.total + it.first + row] = m * ATTN_LN2 + logf(l);
     }
   }
-  end(s, P, 256);
+  end(s, P, COLUMNS);
 }
 
 // ------------------------------------------------------------------------------------------ backward
@@ -566,7 +579,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
   // all before it is done); the wait at the end makes sure that this one does not end first.  The dK, dV kernel's CTAs may come as
   // soon as the last ones of this grid have begun.
   pdl_trigger();
-  begin(s, P, STAGES, WARPS, WARPS - 1, 4 * TN);
+  begin(s, P, STAGES, WARPS, WARPS, 1, WARPS, 4 * TN);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t ts = s.tmem, tdp = ts + TN, tdq = ts + 2 * TN, tq = tdq + 64 * DC, tdo = tq + 32 * DC;
   static_assert(2 * TN + 128 * DC == 4 * TN, "all columns");
@@ -675,20 +688,20 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
           scores(j + 1);
           if (!ok) break;
         }
-        if (j == 0) ok = warp_wait(&s.acc_empty, (n & 1) ^ 1, ab, status);
+        if (j == 0) ok = warp_wait(&s.acc_empty[0], (n & 1) ^ 1, ab, status);
         ok = ok && warp_wait(&s.ready[0], made & 1, ab, status);
         if (!ok) break;
         tc_fence_after();
         if (leader) {
           product_rows<DC, TN, 0, TN / 16>(tdq, tdp, 64, smem_u32(ring + k_now * TILE), j != 0);
           umma_commit(&s.empty[k_now]);
-          if (j == tiles - 1) umma_commit(&s.done);
+          if (j == tiles - 1) umma_commit(&s.done[0]);
         }
         if (j + 1 < tiles) dscores(j + 1);
         if (!ok) break;
       }
     }
-    if (leader && *ab) drain_products(&s.drain, ab, status);
+    if (leader && *ab) drain_products(&s.drain[0], ab, status);
   } else {
     const int part = warp >> 2, in = (warp & 3) * 32 + lane;     // columns part * 64 ..; row of the tile
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
@@ -775,7 +788,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         tc_fence_before();
         warp_arrive(&s.ready[0]);
       }
-      ok = ok && warp_wait(&s.done, n & 1, ab, status);
+      ok = ok && warp_wait(&s.done[0], n & 1, ab, status);
       if (!ok) break;
       tc_fence_after();
       // the next tile's first products run while this one's rows are stored, 64 columns by a warp
@@ -787,7 +800,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
       const int warp_row = prev.t0 + (warp & 3) * 32;
       store_rows<1>(tdq + lanes + part * 64, x, (int64_t)prev.first + warp_row, prev.head, C.dim - part * 64, prev.len - warp_row, C.scale);
       tc_fence_before();
-      warp_arrive(&s.acc_empty);
+      warp_arrive(&s.acc_empty[0]);
     }
   }
   pdl_wait();
@@ -808,7 +821,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
   Shared& s = *reinterpret_cast<Shared*>(s_rows + 2 * (TN / 64) * 128);
   const AttnCall& C = P.c;
   if (!in_place(smem, C.seqs.status)) return;
-  begin(s, P, STAGES, WARPS, 0, 4 * TN);
+  begin(s, P, STAGES, WARPS, WARPS, 1, 1, 4 * TN);
   pdl_wait();                            // delta comes from the dQ kernel
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t ts = s.tmem, tdp = ts + TN, tdv = ts + 2 * TN, tdk = tdv + 64 * DC;
@@ -894,7 +907,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
       dscores(0);
       if (!ok) break;
       for (int i = 0; i < steps; ++i, ++made) {
-        if (i == 0) ok = warp_wait(&s.acc_empty, (n & 1) ^ 1, ab, status);
+        if (i == 0) ok = warp_wait(&s.acc_empty[0], (n & 1) ^ 1, ab, status);
         ok = ok && warp_wait(&s.ready[0], made & 1, ab, status);
         if (!ok) break;
         tc_fence_after();
@@ -913,13 +926,13 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         if (leader) {
           product_rows<DC, TN, 0, TN / 16>(tdk, tdp, 64, smem_u32(ring + q * TILE), i != 0);
           umma_commit(&s.empty[q]);
-          if (i == steps - 1) umma_commit(&s.done);
+          if (i == steps - 1) umma_commit(&s.done[0]);
         }
         if (i + 1 < steps) dscores(i + 1);
         if (!ok) break;
       }
     }
-    if (leader && *ab) drain_products(&s.drain, ab, status);
+    if (leader && *ab) drain_products(&s.drain[0], ab, status);
   } else {
     const int part = warp >> 2;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
@@ -1001,7 +1014,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         warp_arrive(&s.ready[1]);
         if (i + 1 < steps) keep(made + 1, ahead);
       }
-      ok = ok && warp_wait(&s.done, n & 1, ab, status);
+      ok = ok && warp_wait(&s.done[0], n & 1, ab, status);
       if (!ok) break;
       // with eight warps one half stores dV, the other dK
       tc_fence_after();
@@ -1010,7 +1023,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         store_rows<DC>((which == 0 ? tdv : tdk) + lanes, which == 0 ? C.dv : C.dk, (int64_t)it.first + warp_row, it.head, C.dim,
                        it.len - warp_row, which == 0 ? 1.0f : C.scale);
       tc_fence_before();
-      warp_arrive(&s.acc_empty);
+      warp_arrive(&s.acc_empty[0]);
     }
   }
   end(s, P, 4 * TN);
@@ -1030,7 +1043,7 @@ bool addressable(const Strided& x, int heads, int total) {
          x.token < (1ll << 36) && x.head < (1ll << 36);
 }
 // shared memory beside the Shared struct
-template <int DC> constexpr int FWD_BYTES = DC * (CHUNK<128> + FWD_STAGES<DC> * CHUNK<FWD_TN>);
+template <int DC, int HEADS> constexpr int FWD_BYTES = DC * (HEADS * CHUNK<128> + FWD_STAGES<DC, HEADS> * CHUNK<FWD_TN>);
 template <int DC> constexpr int DQ_BYTES = DC * ((DC == 1 ? 3 : 2) * CHUNK<128> + BWD_STAGES<DC> * CHUNK<TN_OF<DC>> + 512) + 1024;
 template <int DC> constexpr int DKV_BYTES = DC * (2 * CHUNK<128> + BWD_STAGES<DC> * CHUNK<TN_OF<DC>>) + 2 * (TN_OF<DC> / 64) * 512;
 
@@ -1063,8 +1076,9 @@ cudaError_t attn_umma_prepare() {
   auto room = [](const void* kernel, int bytes) {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes + (int)sizeof(Shared));
   };
-  cudaError_t e = room((const void*)attn_fwd_kernel<1>, FWD_BYTES<1>);
-  if (e == cudaSuccess) e = room((const void*)attn_fwd_kernel<2>, FWD_BYTES<2>);
+  cudaError_t e = room((const void*)attn_fwd_kernel<1, 1>, FWD_BYTES<1, 1>);
+  if (e == cudaSuccess) e = room((const void*)attn_fwd_kernel<2, 1>, FWD_BYTES<2, 1>);
+  if (e == cudaSuccess) e = room((const void*)attn_fwd_kernel<2, 2>, FWD_BYTES<2, 2>);
   if (e == cudaSuccess) e = room((const void*)attn_dq_kernel<1>, DQ_BYTES<1>);
   if (e == cudaSuccess) e = room((const void*)attn_dq_kernel<2>, DQ_BYTES<2>);
   if (e == cudaSuccess) e = room((const void*)attn_dkv_kernel<1>, DKV_BYTES<1>);
@@ -1088,8 +1102,9 @@ cudaError_t launch_attn_umma_fwd(const Attn* a, const AttnCall& c, cudaStream_t 
       !attn_map(&mv, c.v, c.heads_kv, c.dim, total, FWD_TN))
     return cudaErrorInvalidValue;
   const long tiles = tile_bound(total, c.seqs.N, 128) * c.heads_q;
-  return c.dim <= 64 ? run(attn_fwd_kernel<1>, false, 0, FWD_BYTES<1>, FWD_THREADS, 2, tiles, a, c, st, mq, mk, mv)
-                     : run(attn_fwd_kernel<2>, false, 0, FWD_BYTES<2>, FWD_THREADS, 2, tiles, a, c, st, mq, mk, mv);
+  if (c.dim <= 64) return run(attn_fwd_kernel<1, 1>, false, 0, FWD_BYTES<1, 1>, FWD_THREADS<1>, 2, tiles, a, c, st, mq, mk, mv);
+  if (c.group % 2 != 0) return run(attn_fwd_kernel<2, 1>, false, 0, FWD_BYTES<2, 1>, FWD_THREADS<1>, 2, tiles, a, c, st, mq, mk, mv);
+  return run(attn_fwd_kernel<2, 2>, false, 0, FWD_BYTES<2, 2>, FWD_THREADS<2>, 1, tiles / 2, a, c, st, mq, mk, mv);
 }
 
 cudaError_t launch_attn_umma_bwd(const Attn* a, const AttnCall& c, cudaStream_t st) {
