@@ -117,7 +117,7 @@ int vcas_loss_status(vcas_loss l, int32_t* status);
 /* ------------------------------------------------------------------------------------- optimizer step ---- */
 /*
  * AdamW over any number of tensors.  With g' = g * *grad_scale, per element, every operation rounded to fp32 on its own
- * (with 8-bit states the root and the quotient are good to 2^-22 relative):
+ * (with 8-bit states the quotient is good to 2^-22 relative):
  *   m <- beta1 m + (1 - beta1) g',   v <- beta2 v + (1 - beta2) g' g',
  *   p <- p (1 - lr wd) - (m lr / (1 - beta1^step)) / (sqrt(v) / sqrt(1 - beta2^step) + eps).
  * state_bits 32: m and v are fp32.  state_bits 8: m and r = sqrt(v) are held as e4m3 values, one fp32 scale for each 256

@@ -212,8 +212,9 @@ __device__ __forceinline__ void p_and_ds(const AttnCall& C, const Place& p, int 
     for (int j = 0; j < 4; ++j) {
       const int row = i0 + ty * 4 + i, col = j0 + tx + 16 * j;
       const bool see = row < p.len && col < p.len && (!C.causal || col <= row);
-      s[i][j] = see ? attn_exp2(s[i][j] * c - lse[i]) : 0.f;
-      dp[i][j] = see ? s[i][j] * (dp[i][j] - delta[i]) : 0.f;
+      const bool alone = C.causal ? row == 0 : p.len == 1;       // one key: P = 1, dS = 0
+      s[i][j] = !see ? 0.f : alone ? 1.f : attn_exp2(s[i][j] * c - lse[i]);
+      dp[i][j] = see && !alone ? s[i][j] * (dp[i][j] - delta[i]) : 0.f;
     }
 }
 // lse in units of log 2, and delta, of this thread's rows

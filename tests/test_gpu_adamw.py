@@ -80,8 +80,8 @@ def eight_bit(n, off, seed, pd=F32, gd=F32, copy=True):
 @pytest.mark.parametrize("gd", [F32, BF16])
 @pytest.mark.parametrize("off", [0, 1])
 def test_8_bit_states(pd, gd, off):
-    """Several steps: p from the states held before the step; each new state is an e4m3 neighbour of the exact value.  Root and
-    quotient are each good to 2^-22: the update to 2^-21, with a rounding of p behind it."""
+    """Several steps: p from the states held before the step; each new state is an e4m3 neighbour of the exact value.  The
+    quotient is good to 2^-22 and the root to a rounding: the update to 2^-21, with a rounding of p behind it."""
     entries = [eight_bit(n, off, 20 * i, pd, gd) for i, n in enumerate(SIZES)]
     grid = torch.arange(127, dtype=torch.uint8).view(E4M3).float()            # 0 .. 448, ascending
     opt = vb.AdamW(entries)

@@ -358,3 +358,41 @@ def test_score_range_that_a_first_tile_does_not_show():
             o, lse = op.fwd(q, k, v, starts)
             check(o, ref["o"], what="o")
             check(lse, ref["lse"], what="lse")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("D", [64, 128])
+def test_one_key_has_no_gradient(dtype, D):
+    """A row that sees one key has P = 1 and dS = 0, not what is left of two roundings."""
+    T = 37
+    q, k, v = tensors(T, 4, 2, D, dtype, "plain", 60)
+    do = tensors(T, 4, 2, D, dtype, "plain", 61)[0]
+    starts = packed([1] * T)
+    for causal in (False, True):
+        op = vb.Attention(T, T, 4, 2, D, dtype, causal=causal)
+        o, lse = op.fwd(q, k, v, starts)
+        dq, dk, dv = op.bwd(do, q, k, v, o, lse, starts)
+        assert (dq == 0).all() and (dk == 0).all()
+        assert torch.equal(o, v.repeat_interleave(2, 1))
+        check(dv, reference(q, k, v, starts, causal, D ** -0.5, do)["dv"], what="dv")
+    op = vb.Attention(T, 1, 4, 2, D, dtype, causal=True)
+    o, lse = op.fwd(q, k, v, packed([T]))
+    assert (op.bwd(do, q, k, v, o, lse, packed([T]))[0][0] == 0).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("T", [2, 5, 20, 64, 128])
+def test_few_keys_do_not_lose_precision_to_the_stored_output(T, D):
+    """delta = rowsum(dO O) carries O's rounding into every dS of a row; rows that see one tile of keys take rowsum(P dP).  In norm:
+    the result's own rounding and that of dS, each half a step at most and 0.58 of that on average, 2^-8 0.58 sqrt 2 = 0.0032."""
+    starts = packed([T] * 8)
+    q, k, v = tensors(8 * T, 4, 2, D, BF16, "plain", 62)
+    do = tensors(8 * T, 4, 2, D, BF16, "plain", 63)[0]
+    for causal in (False, True):
+        op = vb.Attention(8 * T, 8, 4, 2, D, BF16, causal=causal)
+        o, lse = op.fwd(q, k, v, starts)
+        grads = op.bwd(do, q, k, v, o, lse, starts)
+        ref = reference(q, k, v, starts, causal, D ** -0.5, do)
+        for name, got in zip(("dq", "dk", "dv"), grads):
+            want = ref[name][0]
+            assert float((got.double() - want).norm() / want.norm()) <= 0.0032, name
