@@ -8,8 +8,15 @@
 //   forward    S = Q K^T,  P = exp(S - m),  O += P V; O is rescaled only where the maximum has risen by more than 2^8
 //   dQ         rows are queries: S, dP = dO V^T, dS = P (dP - delta), dQ += dS K
 //   dK, dV     rows are keys:    S^T = K Q^T, dV += P^T dO, dP^T = V dO^T, dK += dS^T Q, over all query heads of the group
+// P and dS are rounded to bf16, each by up to 2^-9 of itself.  Over many keys these errors are small beside what O and dQ are rounded by
+// themselves; few keys average little.  So the first tile of rows that see FEW keys or less is multiplied as a sum of two bf16 (`few`),
+// with the low parts in the other half of the scores' columns: outputs of such rows are off by their own rounding alone (0.0017 of
+// their norm, 0.0025 by one product).  8 x 2048 tokens, 32/8 heads of 128, causal: forward 267 -> 271 us; backward over 16 sequences of
+// 1 to 2048: 408 -> 411 us.
 // A tile that reaches past its sequence's end holds rows of the next one (or zeros): their scores are masked, and where such rows
 // would be summed over they are zeroed in shared memory, so that nothing of them, a NaN included, gets in.
+#include <type_traits>
+
 #include "attn.cuh"
 #include "umma.cuh"
 
@@ -103,6 +110,16 @@ __device__ __forceinline__ void load_tile(uint8_t* dst, const CUtensorMap* map, 
 #pragma unroll
   for (int c = 0; c < DC; ++c) tma_load_3d(dst + c * CHUNK<ROWS>, map, 64 * c, head, token, bar);
 }
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&t);
+}
+// What rounding x to the pairs `hi` left, rounded in its turn: the sum of both has 16 bits and more.
+__device__ __forceinline__ void low_parts(const uint32_t (&x)[64], const uint32_t (&hi)[32], uint32_t (&lo)[32]) {
+#pragma unroll
+  for (int i = 0; i < 32; ++i)
+    lo[i] = pack_bf16(__uint_as_float(x[2 * i]) - __uint_as_float(hi[i] << 16), __uint_as_float(x[2 * i + 1]) - __uint_as_float(hi[i] & 0xffff0000u));
+}
 // 64 columns of a row of a tile of 128 rows, as 32 pairs
 __device__ __forceinline__ void read_row(const uint8_t* tile, int row, uint32_t (&v)[32]) {
 #pragma unroll
@@ -125,10 +142,6 @@ __device__ __forceinline__ float row_dot(const uint8_t* tile, int row, const uin
     }
   }
   return s0 + s1;
-}
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  const __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&t);
 }
 // A warp's 32 rows of a [128 x 64 DC] accumulator, times f (each lane its row's), to rows of a tensor; `rows` of them exist.  Four lanes
 // exchange 16-byte pieces of their rows, so that a store instruction writes 64 bytes in a row (a lane writing its own row, 16 bytes of 32
@@ -169,7 +182,10 @@ __device__ __forceinline__ void store_rows(uint32_t taddr, const Strided& x, int
 
 // ----------------------------------------------------------------------------------------- the CTA
 constexpr int MAX_STAGES = 10;
+constexpr int FEW = 64;                              // at most a tile of keys
 struct Item { int first, len, t0, head, any; };      // a tile of 128 rows: its sequence, its first row in there, its head
+// whether the first rows of a sequence see FEW keys or less
+__device__ __forceinline__ bool few_keys(const Item& it, bool causal) { return causal || it.len <= FEW; }
 struct Shared {
   uint64_t full[MAX_STAGES], empty[MAX_STAGES];      // ring of the other side's tiles
   uint64_t item_full[2], item_empty[2];
@@ -336,7 +352,7 @@ __device__ __forceinline__ void drain(Shared& s, const Ring& r, int stages, uint
 // Bound by shared memory: Q is read for each tile of keys (there is no room for it in TMEM), 64-wide products with both operands there
 // take 427 cycles for 256 of arithmetic, and the tiles have to be written too.  Two heads on one copy of K and V save a sixth of
 // that: for heads wider than 64 in groups of an even number (8 x 2048 tokens, 32/8 heads of 128, causal: 282 us by one head, 267
-// by two); narrower ones are bound by their exponentials.  (A part of these as polynomials on the FMA pipe: 298 us for one in eight of
+// by two, both before `few`); narrower ones are bound by their exponentials.  (A part of these as polynomials on the FMA pipe: 298 us for one in eight of
 // the pairs where all by the special function unit took 292; the warps' issue slots were what it cost.)
 constexpr int FWD_TN = 64;
 template <int DC, int HEADS> constexpr int FWD_STAGES = HEADS == 2 ? 10 : DC == 1 ? 8 : 5;
@@ -401,6 +417,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     bool ok = true;
     for (int n = 0; ok && get_item(s, n, status, it); ++n) {
       const int tiles = tiles_of(it);
+      const bool few = it.t0 == 0 && few_keys(it, C.causal);
       ok = warp_wait(&s.own_full, n & 1, ab, status);
       if (!ok) break;
       auto scores = [&](bool last) {
@@ -434,6 +451,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         tc_fence_after();
         if (leader) {
           product_rows<DC, TN, 0, TN / 16>(to, ts + (made & 1) * TN, 0, smem_u32(ring + place * TILE), j != 0);
+          if (j == 0 && few) product_rows<DC, TN, 0, TN / 16>(to, ts + (made & 1) * TN + 32, 0, smem_u32(ring + place * TILE), true);
           umma_commit(&s.empty[place]);
           umma_commit(&s.added[h]);
           if (j == tiles - 1) umma_commit(&s.done[h]);
@@ -502,7 +520,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
           if (!ok) break;
         }
         float sum;
-        auto exps = [&]() {
+        auto exps = [&](auto keep) {
           const uint64_t n2 = pack2(-m, -m);
           uint64_t l2[2] = {0, 0};
           float t[2] = {none, none};
@@ -515,18 +533,29 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
             e1 = attn_exp2(e1);
             l2[i & 1] = add2(l2[i & 1], pack2(e0, e1));
             o[i] = pack_bf16(e0, e1);
+            if constexpr (keep.value) {
+              x[2 * i] = __float_as_uint(e0);
+              x[2 * i + 1] = __float_as_uint(e1);
+            }
           }
           float y0, y1;
           unpack2(add2(l2[0], l2[1]), y0, y1);
           sum = y0 + y1;
           over = fmaxf(t[0], t[1]);
         };
-        exps();
+        if (j == 0 && it.t0 == 0 && few_keys(it, C.causal)) {
+          exps(std::true_type());
+          uint32_t lo[32];
+          low_parts(x, o, lo);
+          tmem_st32(at + 32, lo);
+        } else {
+          exps(std::false_type());
+        }
         if (j != 0 && __any_sync(0xffffffffu, over > 64.0f)) {
           lift(over, over > 64.0f);
           if (!ok) break;
           read();
-          exps();
+          exps(std::false_type());
         }
         l += sum;
         tmem_st32(at, o);
@@ -638,6 +667,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
     bool ok = true;
     for (int n = 0; ok && get_item(s, n, status, it); ++n) {
       const int tiles = tiles_of(it);
+      const bool few = it.t0 == 0 && few_keys(it, C.causal);
       // Q and dO are in TMEM, and O has been read
       ok = warp_wait(&s.taken, n & 1, ab, status);
       if (!ok) break;
@@ -696,6 +726,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         tc_fence_after();
         if (leader) {
           product_rows<DC, TN, 0, TN / 16>(tdq, tdp, 64, smem_u32(ring + k_now * TILE), j != 0);
+          if (j == 0 && few) product_rows<DC, TN, 0, TN / 16>(tdq, tdp + 32, 64, smem_u32(ring + k_now * TILE), true);
           umma_commit(&s.empty[k_now]);
           if (j == tiles - 1) umma_commit(&s.done[0]);
         }
@@ -750,6 +781,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
       const float nl = -lse * ATTN_LOG2E;
       const uint64_t n2 = pack2(nl, nl);
       uint64_t d2 = pack2(-delta, -delta);
+      const bool low = it.t0 == 0 && few_keys(it, C.causal);
       for (int j = 0; j < tiles; ++j, ++made) {
         ok = warp_wait(&s.scores[0], made & 1, ab, status);
         if (!ok) break;
@@ -779,7 +811,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
           tmem_ld64(tdp + lanes + part * 64, b);
           if (j == 0) {
             // Rows that see no more than this tile: delta = rowsum(P dP), free of the rounding of O, which few keys average little
-            // (causal sequences of a few tokens: dQ off by 0.0034 of its norm with rowsum(dO O), 0.0025 so).
+            // (causal sequences of a few tokens: dQ off by 0.0034 of its norm with rowsum(dO O) where 0.0025 is its rounding and that of dS).
             const int seen = C.causal ? min(it.len, row + 1) : it.len;
             const bool here = seen <= TN;
             if (part == 0 && seen == 1) a[0] = 0x3f800000u;        // P = 1, and so dS = 0
@@ -805,13 +837,28 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             // for the dK, dV kernel
             if (part == 0 && row < it.len) C.delta[(int64_t)it.head * C.seqs.total + it.first + row] = delta;
           }
+          auto dscores = [&](auto few) {
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            float s0, s1;
-            unpack2(mul2(pack2(__uint_as_float(a[2 * i]), __uint_as_float(a[2 * i + 1])),
-                         add2(pack2(__uint_as_float(b[2 * i]), __uint_as_float(b[2 * i + 1])), d2)), s0, s1);
-            o[i] = pack_bf16(s0, s1);
-          }
+            for (int i = 0; i < 32; ++i) {
+              float s0, s1;
+              unpack2(mul2(pack2(__uint_as_float(a[2 * i]), __uint_as_float(a[2 * i + 1])),
+                           add2(pack2(__uint_as_float(b[2 * i]), __uint_as_float(b[2 * i + 1])), d2)), s0, s1);
+              o[i] = pack_bf16(s0, s1);
+              if constexpr (few.value) {
+                b[2 * i] = __float_as_uint(s0);
+                b[2 * i + 1] = __float_as_uint(s1);
+              }
+            }
+            if constexpr (few.value) {
+              uint32_t rest[32];
+              low_parts(b, o, rest);
+              tmem_st32(tdp + lanes + part * 64 + 32, rest);
+            }
+          };
+          if (j == 0 && low)
+            dscores(std::true_type());
+          else
+            dscores(std::false_type());
         }
         tmem_st32(tdp + lanes + part * 64, o);
         tmem_wait_st();
@@ -861,7 +908,14 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
   auto first_tile = [&](const Item& it) { return C.causal ? it.t0 / TN : 0; };
   auto per_head = [&](const Item& it) { return (it.len + TN - 1) / TN - first_tile(it); };
   struct Step { int head, row; };
-  auto step_of = [&](const Item& it, int i, int per) { return Step{it.head * C.group + i / per, (first_tile(it) + i % per) * TN}; };
+  auto first_step = [&](const Item& it) { return Step{it.head * C.group, first_tile(it) * TN}; };
+  auto advance = [&](const Item& it, Step& st) {
+    st.row += TN;
+    if (st.row >= it.len) {
+      st.row = first_tile(it) * TN;
+      ++st.head;
+    }
+  };
 
   if (warp == WARPS + 1) {
     const Order order(C.seqs, lane, C.causal, true);
@@ -883,11 +937,12 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         load_tile<DC, 128>(sv, &mv, it.head, it.first + it.t0, &s.own_full);
       }
       ++own;
-      const int per = per_head(it), steps = per * C.group;
+      const int steps = per_head(it) * C.group;
       const bool stall = P.stall_once && blockIdx.x == 0 && n == 0;
+      Step st = first_step(it);
       for (int i = 0; i < 2 * steps && ok; ++i) {
-        const Step st = step_of(it, i >> 1, per);
         ok = fill<DC, TN>(s, r, STAGES, ring, (i & 1) ? &mdo : &mq, st.head, it.first + st.row, stall && i == 0, status);
+        if (i & 1) advance(it, st);
       }
       if (!ok) break;
     }
@@ -899,12 +954,14 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     uint32_t made = 0;
     bool ok = true;
     for (int n = 0; ok && get_item(s, n, status, it); ++n) {
-      const int per = per_head(it), steps = per * C.group;
+      const int steps = per_head(it) * C.group;
       ok = warp_wait(&s.own_full, n & 1, ab, status);
       if (!ok) break;
       int q_next = 0, g_next = 0;        // ring places of the next step's Q and dO
-      auto arrived = [&](int i) {
-        const int place = r.stage, have = it.len - step_of(it, i, per).row;
+      Step st = first_step(it);          // the step whose scores were issued last
+      const bool low = few_keys(it, C.causal);
+      auto arrived = [&]() {
+        const int place = r.stage, have = it.len - st.row;
         ok = warp_wait(&s.full[place], r.phase, ab, status);
         if (ok && have < TN) {
           zero_rows<DC, TN>(ring + place * TILE, have, lane);
@@ -915,8 +972,8 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         tc_fence_after();
         return place;
       };
-      auto scores = [&](int i) {
-        q_next = arrived(i);
+      auto scores = [&]() {
+        q_next = arrived();
         if (!ok) return;
         if (leader) {
           product_tiles<DC, TN>(ts, smem_u32(sk), smem_u32(ring + q_next * TILE));
@@ -924,7 +981,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         }
       };
       auto dscores = [&](int i) {
-        g_next = arrived(i);
+        g_next = arrived();
         if (!ok) return;
         if (leader) {
           product_tiles<DC, TN>(tdp, smem_u32(sv), smem_u32(ring + g_next * TILE));
@@ -932,11 +989,12 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
           if (i == steps - 1) umma_commit(&s.own_empty);
         }
       };
-      scores(0);
+      scores();
       if (!ok) break;
       dscores(0);
       if (!ok) break;
       for (int i = 0; i < steps; ++i, ++made) {
+        const bool few = low && st.row == 0;
         if (i == 0) ok = warp_wait(&s.acc_empty[0], (n & 1) ^ 1, ab, status);
         ok = ok && warp_wait(&s.ready[0], made & 1, ab, status);
         if (!ok) break;
@@ -944,10 +1002,12 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         const int q = q_next, g = g_next;
         if (leader) {
           product_rows<DC, TN, 0, TN / 16>(tdv, ts, 64, smem_u32(ring + g * TILE), i != 0);
+          if (few) product_rows<DC, TN, 0, TN / 16>(tdv, ts + 32, 64, smem_u32(ring + g * TILE), true);
           umma_commit(&s.empty[g]);
         }
         if (i + 1 < steps) {
-          scores(i + 1);
+          advance(it, st);
+          scores();
           if (!ok) break;
         }
         ok = warp_wait(&s.ready[1], made & 1, ab, status);
@@ -955,6 +1015,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         tc_fence_after();
         if (leader) {
           product_rows<DC, TN, 0, TN / 16>(tdk, tdp, 64, smem_u32(ring + q * TILE), i != 0);
+          if (few) product_rows<DC, TN, 0, TN / 16>(tdk, tdp + 32, 64, smem_u32(ring + q * TILE), true);
           umma_commit(&s.empty[q]);
           if (i == steps - 1) umma_commit(&s.done[0]);
         }
@@ -972,10 +1033,10 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     uint32_t made = 0;
     bool ok = true;
     for (int n = 0; ok && get_item(s, n, status, it); ++n) {
-      const int per = per_head(it), steps = per * C.group, warp_row = it.t0 + (warp & 3) * 32, row = warp_row + lane;
+      const int steps = per_head(it) * C.group, warp_row = it.t0 + (warp & 3) * 32, row = warp_row + lane;
       // Negative lse (in units of log 2) and delta of a step's 64 queries, for the four warps of this half: a warp brings 16 of them.
-      auto fetch = [&](int i) -> float {
-        const Step st = step_of(it, i, per);
+      Step st = first_step(it), ahead_st = st;
+      auto fetch = [&](const Step& st) -> float {
         const int t = st.row + part * 64 + (warp & 3) * 16 + (lane & 15);
         const int64_t at = (int64_t)st.head * C.seqs.total + it.first + t;
         return t >= it.len ? 0.f : lane < 16 ? C.lse[at] : C.delta[at];
@@ -984,14 +1045,15 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         s_rows[((k & 1) * (TN / 64) + part) * 128 + (lane >> 4) * 64 + (warp & 3) * 16 + (lane & 15)] = lane < 16 ? -f * ATTN_LOG2E : -f;
         warp_arrive(&s.rows_full[part][k & 1]);
       };
-      keep(made, fetch(0));
-      for (int i = 0; i < steps; ++i, ++made) {
-        const float ahead = i + 1 < steps ? fetch(i + 1) : 0.f;
+      keep(made, fetch(st));
+      auto step = [&](int i, auto few) -> bool {
+        advance(it, ahead_st);
+        const float ahead = i + 1 < steps ? fetch(ahead_st) : 0.f;
         const float* mine = s_rows + ((made & 1) * (TN / 64) + part) * 128;
         ok = warp_wait(&s.rows_full[part][made & 1], (made >> 1) & 1, ab, status) && warp_wait(&s.scores[0], made & 1, ab, status);
-        if (!ok) break;
+        if (!ok) return false;
         tc_fence_after();
-        const int base = step_of(it, i, per).row + part * 64;      // first query of this warp's columns
+        const int base = st.row + part * 64;                       // first query of this warp's columns
         const bool cut = it.len - base < 64 || (C.causal && base < it.t0 + 128);
         const int lo = C.causal ? row - base : 0, hi = it.len - base;    // the columns that look at this key
         uint32_t a[64];
@@ -1016,12 +1078,17 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
 #pragma unroll
         for (int e = 0; e < 32; ++e) o[e] = pack_bf16(__uint_as_float(a[2 * e]), __uint_as_float(a[2 * e + 1]));
         tmem_st32(ts + lanes + part * 64, o);
+        if constexpr (few.value) {
+          uint32_t rest[32];
+          low_parts(a, o, rest);
+          tmem_st32(ts + lanes + part * 64 + 32, rest);
+        }
         tmem_wait_st();
         tc_fence_before();
         warp_arrive(&s.ready[0]);
         if (base == 0 && (C.causal || it.len == 1)) a[0] = 0u;     // a query that sees one key: dS = 0
         ok = warp_wait(&s.dscores, made & 1, ab, status);
-        if (!ok) break;
+        if (!ok) return false;
         tc_fence_after();
         {
           uint32_t b[64];
@@ -1036,7 +1103,16 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
               unpack2(mul2(pack2(__uint_as_float(a[x]), __uint_as_float(a[x + 1])),
                            add2(pack2(__uint_as_float(b[x]), __uint_as_float(b[x + 1])), h == 0 ? pack2(f.x, f.y) : pack2(f.z, f.w))), s0, s1);
               o[e + h] = pack_bf16(s0, s1);
+              if constexpr (few.value) {
+                b[x] = __float_as_uint(s0);
+                b[x + 1] = __float_as_uint(s1);
+              }
             }
+          }
+          if constexpr (few.value) {
+            uint32_t rest[32];
+            low_parts(b, o, rest);
+            tmem_st32(tdp + lanes + part * 64 + 32, rest);
           }
         }
         tmem_st32(tdp + lanes + part * 64, o);
@@ -1044,7 +1120,12 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         tc_fence_before();
         warp_arrive(&s.ready[1]);
         if (i + 1 < steps) keep(made + 1, ahead);
-      }
+        st = ahead_st;
+        return true;
+      };
+      const bool low = few_keys(it, C.causal);
+      for (int i = 0; ok && i < steps; ++i, ++made)
+        ok = low && st.row == 0 ? step(i, std::true_type()) : step(i, std::false_type());
       ok = ok && warp_wait(&s.done[0], n & 1, ab, status);
       if (!ok) break;
       // with eight warps one half stores dV, the other dK

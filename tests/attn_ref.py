@@ -6,6 +6,8 @@ they enter a product, and the result once; sums, scores and exponentials are fp3
     `g` = 2^-24 (D + 8) max(s sum |q||k|) + 2^-21 (the latter for the exponential itself), the normalised one by 2 g;
   - a sum of n terms adds n 2^-24 of the sum of absolute terms;
   - delta = rowsum(dO O) inherits the rounding of the stored O: u sum |dO||O|, and its own sum's D 2^-24.
+With `parts` = 2 the bounds are those of P and dS as sums of two numbers of the layer's type, the second the first's rounding error
+(u of it) rounded in its turn, so that u^2 is left, and of delta = rowsum(P dP), which has P's factor and the errors of the two sums.
 """
 import torch
 
@@ -21,11 +23,11 @@ def _one(q, k, v, causal, scale):
     return torch.exp(S - lse[:, None]), lse
 
 
-def reference(q, k, v, starts, causal, scale, do=None, alive=None):
+def reference(q, k, v, starts, causal, scale, do=None, alive=None, parts=1):
     """Returns {name: (value, bound)} of o and lse, and with do of dq, dk, dv (those of `alive` sequences only; the others 0)."""
     dt = q.dtype
     u = torch.finfo(dt).eps / 2
-    uP = u if dt != torch.float32 else 0.0          # P and dS stay in fp32 there
+    uP = u ** parts if dt != torch.float32 else 0.0          # P and dS stay in fp32 there
     q, k, v = q.double(), k.double(), v.double()
     Hq, Hk, D = q.shape[1], k.shape[1], q.shape[2]
     zeros = lambda x: (torch.zeros_like(x), torch.zeros_like(x))
@@ -58,6 +60,9 @@ def reference(q, k, v, starts, causal, scale, do=None, alive=None):
             dS = P * (dP - (dO * O).sum(1)[:, None])
             # off by: P's factor, delta (O's own rounding and its sum), dP's sum
             e_delta = (u * 1.01 + D * F) * (dO.abs() * O.abs()).sum(1)
+            if parts == 2:
+                e_delta = (3 * g + (L + D + 4) * F) * (P * (dO.abs() @ V.abs().T)).sum(1)
+                delta = (dO * O).sum(1)
             e_dS = P * ((3 * g) * (dP - delta[:, None]).abs() + e_delta[:, None] + (D + 2) * F * (dO.abs() @ V.abs().T)) + 1.01 * uP * dS.abs()
             add = lambda name, at, value, bound: (out[name][0][at].add_(value), out[name][1][at].add_(bound))
             add("dv", (t, hk), P.T @ dO, (uP * 1.01 + 3 * g + L * F) * (P.T @ dO.abs()))

@@ -396,3 +396,21 @@ def test_few_keys_do_not_lose_precision_to_the_stored_output(T, D):
         for name, got in zip(("dq", "dk", "dv"), grads):
             want = ref[name][0]
             assert float((got.double() - want).norm() / want.norm()) <= 0.0032, name
+
+
+@pytest.mark.parametrize("D", [40, 64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("Hq,Hk", [(2, 2), (4, 1), (3, 1)])
+def test_rows_of_few_keys_have_the_rounding_of_their_result_alone(D, causal, Hq, Hk):
+    lens = [1, 2, 3, 17, 40, 63, 64]
+    starts = packed(lens)
+    total = sum(lens)
+    q, k, v = tensors(total, Hq, Hk, D, BF16, "plain", 3)
+    do = tensors(total, Hq, Hk, D, BF16, "plain", 4)[0]
+    op = vb.Attention(total, len(lens), Hq, Hk, D, BF16, causal=causal)
+    ref = reference(q, k, v, starts, causal, 1.0 / math.sqrt(D), do, parts=2)
+    o, lse = op.fwd(q, k, v, starts)
+    check(o, ref["o"], what="o")
+    grads = op.bwd(do, q, k, v, ref["o"][0].to(BF16), ref["lse"][0].float(), starts)
+    for name, x in zip(("dq", "dk", "dv"), grads):
+        check(x, ref[name], what=name)
