@@ -4,8 +4,8 @@
 // bytes of fp32, 16 of bf16, 8 of e4m3), and the whole table of tensors travels in the kernel's parameters, so that a step
 // neither copies a table to the device nor keeps one there.  A warp's 256 elements are the block of an 8-bit state's scale: its
 // largest value is one warp reduction, on the bits as integers, which carry a NaN along.
-// Every multiplication and addition is rounded on its own (no contraction to fma; two elements an instruction): with 32-bit states
-// the update is then the same to the bit wherever it is computed from the formulas.
+// The states' multiplications and additions are rounded one by one (no contraction to fma), with 32-bit states all of the update's: it is
+// then the same to the bit wherever it is computed from the formulas.
 #include <cmath>
 
 #include <cuda_fp16.h>
@@ -17,8 +17,10 @@
 namespace vcas {
 namespace {
 
-constexpr int THREADS = 256;
-constexpr int CHUNK = THREADS * 8;       // elements a CTA works on
+// 8-bit states need arithmetic between their loads and stores, and smaller CTAs mix these better (314 M elements: 512 threads 914 us, 256
+// 880, 128 862; several chunks by one CTA, which saves finding the tensor, 916 and more).
+template <int BITS> constexpr int THREADS = BITS == 8 ? 128 : 256;
+template <int BITS> constexpr int CHUNK = THREADS<BITS> * 8;       // elements a CTA works on
 
 struct Entry {
   void* p; const void* g; void* m; void* v; float* m_scale; float* v_scale; void* copy;
@@ -110,15 +112,6 @@ __device__ __forceinline__ void singles(const Eight& e, float (&f)[8]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) unpack2(e.p[i], f[2 * i], f[2 * i + 1]);
 }
-// Products that are added to something are made one by one: mul.f32x2 in front of add.f32x2 became one fma, with a rounding less.
-__device__ __forceinline__ Eight times(const Eight& a, float by) {
-  float x[8];
-  singles(a, x);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = __fmul_rn(x[i], by);
-  return pairs(x);
-}
-// the others
 __device__ __forceinline__ Eight scaled(const Eight& a, float by) {
   const uint64_t b = pack2(by, by);
   Eight e;
@@ -126,10 +119,26 @@ __device__ __forceinline__ Eight scaled(const Eight& a, float by) {
   for (int i = 0; i < 4; ++i) e.p[i] = mul2(a.p[i], b);
   return e;
 }
-__device__ __forceinline__ Eight plus(const Eight& a, const Eight& b) {
+__device__ __forceinline__ Eight square(const Eight& a) {
   Eight e;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) e.p[i] = add2(a.p[i], b.p[i]);
+  for (int i = 0; i < 4; ++i) e.p[i] = mul2(a.p[i], a.p[i]);
+  return e;
+}
+// Sums of products are made one by one: mul.f32x2 in front of add.f32x2 became one fma, with a rounding less.
+__device__ __forceinline__ Eight plus(const Eight& a, const Eight& b) {
+  float x[8], y[8];
+  singles(a, x);
+  singles(b, y);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = __fadd_rn(x[i], y[i]);
+  return pairs(x);
+}
+__device__ __forceinline__ Eight times_plus(const Eight& a, float by, const Eight& b) {
+  const uint64_t k = pack2(by, by);
+  Eight e;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) e.p[i] = fma2(a.p[i], k, b.p[i]);
   return e;
 }
 
@@ -148,22 +157,25 @@ __device__ __forceinline__ Eight decode(uint2 c, float scale) {
 }
 // A value times 2^-120 has its e4m3 exponent and mantissa in bits 20-26, subnormals included; what is below them decides together with the
 // random bits (in bits 12-19, and half of their step) whether the code goes up by one.  BYTE: of each element's halfword.
-// POSITIVE: no signs, and a positive value does not become 0.
+// POSITIVE: no signs, and a positive value does not become 0.  A value may come out up to 3 steps of fp32 above 448, too few to
+// reach the next code: what is added is at most 2^20 - 2048.
+__device__ __forceinline__ uint32_t largest(uint32_t top, float a, float b) {
+  float r;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(__uint_as_float(top)), "f"(a), "f"(b));
+  return __float_as_uint(r);
+}
 template <bool POSITIVE, int BYTE>
 __device__ __forceinline__ uint2 encode(const float (&f)[8], const uint32_t (&rnd)[4], float* scale_at, int lane) {
   uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) top = max(top, POSITIVE ? __float_as_uint(f[i]) : __float_as_uint(f[i]) & 0x7fffffffu);
+  for (int i = 0; i < 8; i += 2) top = largest(top, f[i], f[i + 1]);
   const float big = __uint_as_float(__reduce_max_sync(0xffffffffu, top));
   if (lane == 0) *scale_at = __fmul_rn(big, 1.0f / 448.0f);
   // under 2^-100 (sqrt(v) is never that small) 1 / big would leave fp32's range: such an m is held as 0
   const float inv = big >= 0x1p-100f ? __fmul_rn(__frcp_rn(big), 448.0f) : 0.f;
   uint32_t w[2] = {0, 0};
-  float y[8], z[8];
-  singles(scaled(pairs(f), inv), y);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] = fminf(fabsf(y[i]), 448.0f);
-  singles(scaled(pairs(y), 0x1p-120f), z);
+  float z[8];
+  singles(scaled(scaled(pairs(f), inv), 0x1p-120f), z);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     // bytes 0, 0, random, 0x80: shifted left by 4 that is the random byte in bits 12-19 and 2048
@@ -177,11 +189,21 @@ __device__ __forceinline__ uint2 encode(const float (&f)[8], const uint32_t (&rn
   return make_uint2(w[0], w[1]);
 }
 
-// sqrt(x), rounded correctly but for the rarest x: x / sqrt(x) and one step of Newton's iteration on its exact residual.
+// sqrt(x), rounded correctly but for the rarest x: x / sqrt(x) and one step of Newton's iteration on its exact residual.  x under fp32's
+// normal numbers counts as the least of them: the approximation would take it for 0.
 __device__ __forceinline__ float root_of(float x) {
-  const float r = rsqrtf(x), s = __fmul_rn(x, r);
-  const float better = fmaf(fmaf(-s, s, x), 0.5f * r, s);
+  const float y = fmaxf(x, 0x1p-126f);
+  float r;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(y));
+  const float s = __fmul_rn(y, r);
+  const float better = fmaf(fmaf(-s, s, y), 0.5f * r, s);
   return x > 0.f ? better : x;           // 0, and what is no number
+}
+// 1 / x, good to an ulp, of a normal x
+__device__ __forceinline__ float reciprocal(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
 }
 
 __device__ __forceinline__ void philox(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t k0, uint32_t k1, uint32_t (&out)[4]) {
@@ -197,7 +219,7 @@ __device__ __forceinline__ void philox(uint32_t c0, uint32_t c1, uint32_t c2, ui
 }
 
 template <typename P, typename G, int BITS, int CAP>
-__global__ void __launch_bounds__(THREADS, BITS == 8 ? 6 : 4) adamw_kernel(const __grid_constant__ Table<CAP> t) {
+__global__ void __launch_bounds__(THREADS<BITS>, BITS == 8 ? 12 : 4) adamw_kernel(const __grid_constant__ Table<CAP> t) {
   // the tensor this chunk belongs to: the last one that begins at or before it
   int lo = 0, hi = t.count - 1;
   while (lo < hi) {
@@ -215,7 +237,7 @@ __global__ void __launch_bounds__(THREADS, BITS == 8 ? 6 : 4) adamw_kernel(const
   if (t.grad_scale != nullptr) scale_g = *t.grad_scale;
   uint32_t k0 = t.seed_lo, k1 = t.seed_hi;
   if (BITS == 8 && t.seed_dev != nullptr) { const uint64_t s = *t.seed_dev; k0 = (uint32_t)s; k1 = (uint32_t)(s >> 32); }
-  const int64_t at = (int64_t)(blockIdx.x - e.first) * CHUNK + threadIdx.x * 8;
+  const int64_t at = (int64_t)(blockIdx.x - e.first) * CHUNK<BITS> + threadIdx.x * 8;
   const int64_t left = e.n - at;
   const int have = left >= 8 ? 8 : left > 0 ? (int)left : 0;
   // a whole warp without elements has nothing to do; the others keep all lanes for the block's largest value
@@ -245,29 +267,40 @@ __global__ void __launch_bounds__(THREADS, BITS == 8 ? 6 : 4) adamw_kernel(const
   if (BITS == 8) {
     m = decode(mc, ms);
     v = decode(vc, vs);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v.p[i] = mul2(v.p[i], v.p[i]);
+    v = square(v);
   }
-  m = plus(times(m, t.b1), times(g, t.c1));
-  Eight gg;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) gg.p[i] = mul2(g.p[i], g.p[i]);
-  v = plus(times(v, t.b2), times(gg, t.c2));
+  m = plus(scaled(m, t.b1), scaled(g, t.c1));
+  v = plus(scaled(v, t.b2), scaled(square(g), t.c2));
   singles(v, root);
   // 32-bit states: the correctly rounded root and quotient, which HBM leaves time for.  With 8-bit ones, half the bytes, it does
-  // not (314 M elements: 1266 us, now 985): a root in fewer steps, a quotient good to two ulp, which no state depends on.
+  // not (issue slots were 81 % in use at 62 % of its bandwidth): a root in fewer steps, and for p, on which no state depends, a quotient
+  // good to two ulp and fused sums (314 M elements: 1266 us with the former, 862 so).
+  if (BITS == 8) {
+    float denom[8];
+    const float least = t.eps > 0.f ? fmaxf(t.eps, 0x1p-126f) : t.eps;        // denom is normal, or 0 as the formula has it
 #pragma unroll
-  for (int i = 0; i < 8; ++i) root[i] = BITS == 32 ? __fsqrt_rn(root[i]) : root_of(root[i]);
-  float denom[8], step[8];
-  const uint64_t eps = pack2(t.eps, t.eps);
-  Eight d = times(pairs(root), inv);
+    for (int i = 0; i < 8; ++i) {
+      root[i] = root_of(root[i]);
+      denom[i] = least;
+    }
+    singles(times_plus(pairs(root), inv, pairs(denom)), denom);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) d.p[i] = add2(d.p[i], eps);
-  singles(d, denom);
-  singles(scaled(m, step_size), step);
+    for (int i = 0; i < 8; ++i) denom[i] = reciprocal(denom[i]);
+    const Eight step = scaled(m, -step_size), d = pairs(denom);
+    Eight q;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) step[i] = -(BITS == 32 ? __fdiv_rn(step[i], denom[i]) : __fdividef(step[i], denom[i]));
-  singles(plus(times(p, keep), pairs(step)), x);
+    for (int i = 0; i < 4; ++i) q.p[i] = mul2(step.p[i], d.p[i]);
+    singles(times_plus(p, keep, q), x);
+  } else {
+    float step[8], denom[8], kept[8];
+    singles(scaled(m, step_size), step);
+    singles(scaled(p, keep), kept);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      denom[i] = __fadd_rn(__fmul_rn(__fsqrt_rn(root[i]), inv), t.eps);
+      x[i] = __fsub_rn(kept[i], __fdiv_rn(step[i], denom[i]));
+    }
+  }
   store((P*)e.p + at, have, wide, x);
   if (sizeof(P) == 4 && e.copy != nullptr) store((__nv_bfloat16*)e.copy + at, have, wide, x);
   singles(m, x);
@@ -290,7 +323,7 @@ bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; 
 
 template <typename P, typename G, int BITS, int CAP>
 cudaError_t launch(const Table<CAP>& t, uint32_t chunks, cudaStream_t st) {
-  adamw_kernel<P, G, BITS, CAP><<<chunks, THREADS, 0, st>>>(t);
+  adamw_kernel<P, G, BITS, CAP><<<chunks, THREADS<BITS>, 0, st>>>(t);
   return cudaGetLastError();
 }
 template <int CAP>
@@ -321,7 +354,7 @@ int fill(const vcas_adamw_tensor* ts, int n, int cls, int from, double lr, Table
   for (; i < n && t.count < CAP; ++i) {
     const vcas_adamw_tensor& x = ts[i];
     if (x.n == 0 || class_of(x) != cls) continue;
-    const int64_t c = (x.n + CHUNK - 1) / CHUNK;
+    const int64_t chunk = x.state_bits == 8 ? CHUNK<8> : CHUNK<32>, c = (x.n + chunk - 1) / chunk;
     if (*chunks + c > (1u << 30)) break;
     Entry& e = t.e[t.count++];
     e.p = x.p; e.g = x.g; e.m = x.m; e.v = x.v; e.m_scale = x.m_scale; e.v_scale = x.v_scale; e.copy = x.copy;
