@@ -1,10 +1,11 @@
 // Attention over packed sequences on the tensor cores (bf16, tcgen05): one forward and two backward kernels.
 //
 // A CTA stays for as long as there are tiles of 128 rows of one head to be had, and walks each against the tiles of the other
-// side.  One warp takes tiles from a counter and loads with TMA, ahead of the others and across tiles; one lane issues the products;
-// four or eight warps turn scores into probabilities, a row of TMEM being a lane's own.  Scores stay in TMEM; P and dS go back
-// there as bf16, over the scores they came from, and are the A operand of the product that follows.  tcgen05.mma of one thread run in
-// order, so a tile of scores may be overwritten by the next product as soon as the product that reads it is issued.
+// side.  One warp takes tiles from a counter and loads with TMA, ahead of the others and across tiles; one lane of another (in the forward
+// of two heads, of one for each) issues the products; four or eight warps turn scores into probabilities, a row of TMEM being a lane's
+// own.  Scores stay in TMEM; P goes back there as bf16 over S, dS over dP, as the A operand of the product that follows.
+// tcgen05.mma of one thread run in order, so a tile of scores may be overwritten by the next product as soon as the product that
+// reads it is issued.
 //   forward    S = Q K^T,  P = exp(S - m),  O += P V; O is rescaled only where the maximum has risen by more than 2^8
 //   dQ         rows are queries: S, dP = dO V^T, dS = P (dP - delta), dQ += dS K
 //   dK, dV     rows are keys:    S^T = K Q^T, dV += P^T dO, dP^T = V dO^T, dK += dS^T Q, over all query heads of the group
@@ -1158,6 +1159,11 @@ bool addressable(const Strided& x, int heads, int total) {
 template <int DC, int HEADS> constexpr int FWD_BYTES = DC * (HEADS * CHUNK<128> + FWD_STAGES<DC, HEADS> * CHUNK<FWD_TN>);
 template <int DC> constexpr int DQ_BYTES = DC * ((DC == 1 ? 3 : 2) * CHUNK<128> + BWD_STAGES<DC> * CHUNK<TN_OF<DC>> + 512) + 1024;
 template <int DC> constexpr int DKV_BYTES = DC * (2 * CHUNK<128> + BWD_STAGES<DC> * CHUNK<TN_OF<DC>>) + 2 * (TN_OF<DC> / 64) * 512;
+// A CTA of the dK, dV kernel holds TMEM while it waits for the dQ kernel's grid.  It must not come to an SM where that keeps a CTA of
+// the latter from its columns: beside as many as fill TMEM there is no shared memory for it (nor for three of any kind here).
+constexpr int SM_BYTES = 228 * 1024;
+static_assert(BWD_CTAS<1> * DQ_BYTES<1> + DKV_BYTES<1> > SM_BYTES && BWD_CTAS<2> * DQ_BYTES<2> + DKV_BYTES<2> > SM_BYTES, "see above");
+static_assert(3 * DKV_BYTES<1> > SM_BYTES && 3 * FWD_BYTES<1, 1> > SM_BYTES && DKV_BYTES<2> + FWD_BYTES<1, 1> > SM_BYTES, "see above");
 
 template <typename... KArgs, typename... M>
 cudaError_t run(void (*kernel)(KArgs...), bool after, int which, int bytes, int threads, int ctas, long tiles, const Attn* a,
