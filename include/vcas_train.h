@@ -29,7 +29,8 @@ extern "C" {
  *   S = s Q K^T,  causal: S_ij = -inf for j > i,  P = softmax(S) by rows,  O = P V,  lse_i = log sum_j exp(S_ij);
  *   dV = P^T dO,  dP = dO V^T,  dS = P (dP - rowsum(dO O)),  dQ = s dS K,  dK = s dS^T Q,
  * dK and dV summed over the query heads that share them.  Sums, softmax statistics and lse are fp32; in bf16 layers P and dS
- * are rounded to bf16 where they enter a product, O and the gradients once when stored.
+ * are rounded to bf16 where they enter a product (on the tensor cores to a sum of two bf16 where a sequence's first rows, of
+ * 64 keys or less, are concerned), O and the gradients once when stored.
  * A sequence may be empty.  Rows from starts[N] on are neither read nor written.  starts that descend, are negative
  * or pass `total` are not followed: those sequences are left out and vcas_attn_status reports VCAS_ERR_BAD_ARG.
  * A NaN or infinity in a row of q, k or v reaches that sequence's results only.
@@ -46,8 +47,9 @@ typedef struct {
 } vcas_attn_desc;
 
 /* A [total, heads, head_dim] tensor: element (t, h, d) is ptr[t * token + h * head + d] (strides in elements, not
- * negative; q, k, v and their gradients may lie in one buffer, as a joint projection leaves them).  Any alignment of the
- * dtype is served; bf16 with 16-byte aligned ptr and strides that are multiples of 8 runs on the tensor cores. */
+ * negative; q, k, v and their gradients may lie in one buffer, as a joint projection leaves them; a stride of 0 repeats an
+ * input).  What is written overlaps neither itself nor anything else of the call.  Any alignment of the dtype is
+ * served; bf16 with 16-byte aligned ptr and strides that are multiples of 8 runs on the tensor cores. */
 typedef struct {
   void* ptr;
   int64_t token, head;
@@ -117,7 +119,8 @@ int vcas_loss_status(vcas_loss l, int32_t* status);
 /* ------------------------------------------------------------------------------------- optimizer step ---- */
 /*
  * AdamW over any number of tensors.  With g' = g * *grad_scale, per element, every operation rounded to fp32 on its own
- * (with 8-bit states the quotient is good to 2^-22 relative):
+ * (with 8-bit states, p: the quotient is good to 2^-22 relative, its denominator and p's new value are fused sums; v and eps
+ * other than 0 count as no less than 2^-126):
  *   m <- beta1 m + (1 - beta1) g',   v <- beta2 v + (1 - beta2) g' g',
  *   p <- p (1 - lr wd) - (m lr / (1 - beta1^step)) / (sqrt(v) / sqrt(1 - beta2^step) + eps).
  * state_bits 32: m and v are fp32.  state_bits 8: m and r = sqrt(v) are held as e4m3 values, one fp32 scale for each 256
