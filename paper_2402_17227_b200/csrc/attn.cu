@@ -315,35 +315,47 @@ __global__ void __launch_bounds__(THREADS) attn_fma_dkv_kernel(AttnCall C) {
   store_rows<T, DP>(C.dk, p.first, p.len, p.t0, p.head, C.dim, tx, ty, dk, f);
 }
 
-// A warp per token: delta of its heads if its sequence is worked on (DELTA), else zeros in its rows of the gradients.  wide: those rows can be
-// written 16 bytes at a time.
+// A warp for some tokens one behind the other: delta of their heads where the sequence is worked on (DELTA), else zeros in their rows of the
+// gradients.  wide: those rows can be written 16 bytes at a time.
 template <typename T, bool DELTA>
-__global__ void __launch_bounds__(256) attn_rows_kernel(AttnCall C, bool wide) {
+__global__ void __launch_bounds__(256, 8) attn_rows_kernel(AttnCall C, bool wide) {
   pdl_trigger();                         // what follows works on other sequences
-  const int t = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  if (t >= C.seqs.total) return;
   const Seqs& q = C.seqs;
-  // the last sequence that begins at or before t (the empty ones before it begin there too)
-  int lo = 0, hi = q.N - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (q.starts[mid] <= t) lo = mid; else hi = mid - 1;
-  }
-  int first;
-  const int len = seq_length(q, lo, first);
-  if (t < first || t >= first + len) return;
+  const int lane = threadIdx.x & 31, in_cta = (int)(blockDim.x >> 5), warps = (int)gridDim.x * in_cta;
+  const int each = (q.total + warps - 1) / warps;
+  const int64_t from = (int64_t)((int)blockIdx.x * in_cta + (int)(threadIdx.x >> 5)) * each;
+  const int to = (int)min((int64_t)q.total, from + each);
+  // a row of zeros in pieces of 16 bytes: this lane's piece of a head, and its heads mine, mine + at_once, ...
+  constexpr int VN = 16 / sizeof(T);
+  const int per = C.dim / VN, at_once = 32 / per, piece = lane % per, mine = lane / per < at_once ? lane / per : 1 << 20;
+  int first = 0, end = 0;                // the sequence that t lies in, once found
   bool alive = true;
-  if (q.alive != nullptr) {
-    int a = 0, b = seq_count(q);
-    const int count = b;
-    while (a < b) {
-      const int mid = (a + b) >> 1;
-      if (q.alive[mid] < lo) a = mid + 1; else b = mid;
+  for (int t = (int)min((int64_t)q.total, from); t < to; ++t) {
+    if (t < first || t >= end) {
+      // the last sequence that begins at or before t (the empty ones before it begin there too)
+      int lo = 0, hi = q.N - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (q.starts[mid] <= t) lo = mid; else hi = mid - 1;
+      }
+      const int len = seq_length(q, lo, first);
+      end = first + len;
+      if (t < first || t >= end) continue;
+      if (q.alive != nullptr) {
+        int a = 0, b = seq_count(q);
+        const int count = b;
+        while (a < b) {
+          const int mid = (a + b) >> 1;
+          if (q.alive[mid] < lo) a = mid + 1; else b = mid;
+        }
+        alive = a < count && q.alive[a] == lo;
+      }
     }
-    alive = a < count && q.alive[a] == lo;
-  }
-  if (alive) {
-    if (DELTA)
+    if (alive) {
+      if (!DELTA) {
+        t = end - 1;                     // nothing to do up to there
+        continue;
+      }
       for (int h = 0; h < C.heads_q; ++h) {
         const T* o = (const T*)C.o.p + (int64_t)t * C.o.token + (int64_t)h * C.o.head;
         const T* g = (const T*)C.d_o.p + (int64_t)t * C.d_o.token + (int64_t)h * C.d_o.head;
@@ -352,21 +364,22 @@ __global__ void __launch_bounds__(256) attn_rows_kernel(AttnCall C, bool wide) {
         s = warp_sum(s);
         if (lane == 0) C.delta[(int64_t)h * q.total + t] = s;
       }
-  } else if (!C.skip_dropped) {
-    auto zero = [&](const Strided& x, int heads) {
-      T* base = (T*)const_cast<void*>(x.p) + (int64_t)t * x.token;
-      constexpr int VN = 16 / sizeof(T);
-      if (wide) {
-        const int per = C.dim / VN;
-        for (int i = lane; i < heads * per; i += 32)
-          *reinterpret_cast<uint4*>(base + (int64_t)(i / per) * x.head + (i % per) * VN) = make_uint4(0, 0, 0, 0);
-      } else {
-        for (int i = lane; i < heads * C.dim; i += 32) put(base + (int64_t)(i / C.dim) * x.head + i % C.dim, 0.f);
-      }
-    };
-    zero(C.dq, C.heads_q);
-    zero(C.dk, C.heads_kv);
-    zero(C.dv, C.heads_kv);
+    } else if (!C.skip_dropped) {
+      auto zero = [&](const Strided& x, int heads) {
+        T* base = (T*)const_cast<void*>(x.p) + (int64_t)t * x.token;
+        if (wide) {
+          base += mine * x.head + piece * VN;
+          const int64_t step = at_once * x.head;
+#pragma unroll 4
+          for (int h = mine; h < heads; h += at_once, base += step) *reinterpret_cast<uint4*>(base) = make_uint4(0, 0, 0, 0);
+        } else {
+          for (int i = lane; i < heads * C.dim; i += 32) put(base + (int64_t)(i / C.dim) * x.head + i % C.dim, 0.f);
+        }
+      };
+      zero(C.dq, C.heads_q);
+      zero(C.dk, C.heads_kv);
+      zero(C.dv, C.heads_kv);
+    }
   }
 }
 
@@ -435,6 +448,10 @@ cudaError_t attn_fma_prepare() {
   if (e == cudaSuccess) e = room<float, 128>();
   if (e == cudaSuccess) e = room<__nv_bfloat16, 64>();
   if (e == cudaSuccess) e = room<__nv_bfloat16, 128>();
+  // an SM divides its memory anew only when it is idle: as the kernel needs it that is to begin beside this one
+  auto beside = [](const void* k) { return cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared); };
+  if (e == cudaSuccess) e = beside((const void*)attn_rows_kernel<float, false>);
+  if (e == cudaSuccess) e = beside((const void*)attn_rows_kernel<__nv_bfloat16, false>);
   return e;
 }
 cudaError_t launch_attn_fma_fwd(const Attn* a, const AttnCall& c, cudaStream_t st) {
@@ -444,12 +461,16 @@ cudaError_t launch_attn_fma_fwd(const Attn* a, const AttnCall& c, cudaStream_t s
 }
 template <bool DELTA>
 static cudaError_t rows(const Attn* a, const AttnCall& c, cudaStream_t st) {
-  const unsigned grid = (unsigned)((c.seqs.total + 7) / 8);
+  // delta: a warp a token.  Zeros alone are written beside the kernel that follows: one small CTA an SM leaves it its registers, and as
+  // all of them begin at once, so does that kernel (64 x 197 tokens of 12 heads of 64, 40 % kept:
+  // 57.7 us for the whole backward, 64.8 with a warp a token).
+  const int threads = DELTA ? 256 : 128, most = (c.seqs.total + threads / 32 - 1) / (threads / 32);
+  const unsigned grid = (unsigned)(DELTA ? most : (most < a->num_sms ? most : a->num_sms));
   const int elem = a->desc.dtype == VCAS_DTYPE_BF16 ? 2 : 4, vn = 16 / elem;
   auto wide = [&](const Strided& x) { return ((uintptr_t)x.p & 15) == 0 && x.token % vn == 0 && x.head % vn == 0; };
   const bool w = wide(c.dq) && wide(c.dk) && wide(c.dv);
-  if (elem == 2) attn_rows_kernel<__nv_bfloat16, DELTA><<<grid, 256, 0, st>>>(c, w);
-  else attn_rows_kernel<float, DELTA><<<grid, 256, 0, st>>>(c, w);
+  if (elem == 2) attn_rows_kernel<__nv_bfloat16, DELTA><<<grid, threads, 0, st>>>(c, w);
+  else attn_rows_kernel<float, DELTA><<<grid, threads, 0, st>>>(c, w);
   return cudaGetLastError();
 }
 cudaError_t launch_attn_fma_bwd(const Attn* a, const AttnCall& c, cudaStream_t st) {
