@@ -236,3 +236,22 @@ def test_refusals():
     with pytest.raises(ValueError):
         good.step(1, lr=LR, grad_scale=torch.ones(1))
     vb.AdamW([]).step(1, lr=LR)
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-40])
+def test_8_bit_states_of_the_smallest_gradients(eps):
+    """v = (1 - beta2) g^2 under fp32's normal numbers counts as 2^-126, eps (not 0) as no less: the step is finite and that of the formula
+    with them.  Four roundings, an ulp each of root and reciprocal: 2^-20 relative is more than all.  Without a gradient p stays."""
+    n = 512
+    p, g = torch.zeros(n, device="cuda"), torch.full((n,), 1e-20, device="cuda")
+    p[256:], g[256:] = 1.0, 0.0
+    t = vb.AdamWTensor.make(p, g, bits=8)
+    vb.AdamW([t]).step(1, lr=LR, beta1=B1, beta2=B2, eps=eps)
+    m = (1.0 - B1) * 1e-20
+    denom = 2.0 ** -63 / math.sqrt(1.0 - B2) + (2.0 ** -126 if eps else 0.0)
+    want = -LR / (1.0 - B1) * m / denom
+    assert ((p[:256].double() / want - 1.0).abs() <= 2.0 ** -20).all()
+    if eps:
+        assert (p[256:] == 1.0).all()
+    r = t.v.float() * t.v_scale.repeat_interleave(256)
+    assert (r[256:] == 0).all() and ((r[:256].double() / 2.0 ** -63 - 1.0).abs() <= 2.0 ** -20).all()

@@ -414,3 +414,11 @@ def test_rows_of_few_keys_have_the_rounding_of_their_result_alone(D, causal, Hq,
     grads = op.bwd(do, q, k, v, ref["o"][0].to(BF16), ref["lse"][0].float(), starts)
     for name, x in zip(("dq", "dk", "dv"), grads):
         check(x, ref[name], what=name)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("D", [8, 40, 72, 128])
+@pytest.mark.parametrize("layout", ["plain", "heads", "odd"])
+def test_rows_of_dropped_sequences_become_zero_in_every_layout(dtype, D, layout):
+    lens = [(37 * i * i) % 91 for i in range(40)]        # some empty
+    run(lens, 6, 2, D, dtype, False, layout, alive=list(range(1, 40, 3)), behind=3)
