@@ -746,9 +746,13 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
     uint32_t made = 0, summed = 0;
     Ring r;                              // the loads, to find O among them
     bool ok = true;
-    // the next tile of rows: Q and dO to TMEM, delta
+    // The next tile of rows: Q and dO to TMEM, delta.  s_half: every warp has read what the tile before left there.  It reads delta before
+    // it arrives at a barrier that all of the tile's later steps wait for, but the sums of a single tile of keys as the last.
     auto take = [&](int n) -> bool {
+      const bool single = DC == 2 && n > 0 && tiles_of(it) == 1;
       if (!get_item(s, n, status, it, s_lse + in, &lse)) return false;
+      if (single) ok = warp_wait(&s.sums, summed++ & 1, ab, status);
+      if (!ok) return false;
       ok = warp_wait(&s.own_full, n & 1, ab, status);
       if (!ok) return false;
       uint32_t v[32];
@@ -831,6 +835,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                 ok = warp_wait(&s.sums, summed++ & 1, ab, status);
                 if (!ok) break;
                 t0 = s_half[in] + s_half[128 + in];
+                warp_arrive(&s.sums);            // read; see take
               }
               if (here) delta = t0;
             }
@@ -866,13 +871,14 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         tc_fence_before();
         warp_arrive(&s.ready[0]);
       }
+      if (!ok) break;
+      // the next tile's Q and dO go to TMEM beside the last product (S and dP, for which they were needed, are done), and its first products
+      // run while this one's rows are stored, 64 columns by a warp
+      prev = it;
+      more = take(n + 1);
       ok = ok && warp_wait(&s.done[0], n & 1, ab, status);
       if (!ok) break;
       tc_fence_after();
-      // the next tile's first products run while this one's rows are stored, 64 columns by a warp
-      prev = it;
-      more = take(n + 1);
-      if (!ok) break;
       Strided x = C.dq;
       x.p = (const __nv_bfloat16*)x.p + part * 64;
       const int warp_row = prev.t0 + (warp & 3) * 32;
