@@ -255,3 +255,21 @@ def test_8_bit_states_of_the_smallest_gradients(eps):
         assert (p[256:] == 1.0).all()
     r = t.v.float() * t.v_scale.repeat_interleave(256)
     assert (r[256:] == 0).all() and ((r[:256].double() / 2.0 ** -63 - 1.0).abs() <= 2.0 ** -20).all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_more_elements_than_31_bits_count(bits):
+    """The last elements of 2^31 + 4864 get the step that they get in a tensor of their own."""
+    n, few = (1 << 31) + 4864, 4864
+    p, g = torch.zeros(n, dtype=BF16, device="cuda"), torch.zeros(n, dtype=BF16, device="cuda")
+    p[-few:], g[-few:] = tensor(few, BF16, 0, 1), tensor(few, BF16, 0, 2, scale=1e-2)
+    small, large = (vb.AdamWTensor.make(p[-few:].clone(), g[-few:].clone(), bits, weight_decay=0.1),
+                    vb.AdamWTensor.make(p, g, bits, weight_decay=0.1))
+    vb.AdamW([small]).step(2, lr=LR, beta1=B1, beta2=B2, eps=EPS, seed=3)
+    vb.AdamW([large]).step(2, lr=LR, beta1=B1, beta2=B2, eps=EPS, seed=3)
+    assert torch.equal(large.p[-few:], small.p)
+    if bits == 32:
+        assert torch.equal(large.m[-few:], small.m) and torch.equal(large.v[-few:], small.v)
+    else:
+        assert torch.equal(large.m_scale[-few // 256:], small.m_scale) and torch.equal(large.v_scale[-few // 256:], small.v_scale)
+    assert (large.p[:-few].view(torch.int32) == 0).all()

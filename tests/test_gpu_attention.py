@@ -422,3 +422,31 @@ def test_rows_of_few_keys_have_the_rounding_of_their_result_alone(D, causal, Hq,
 def test_rows_of_dropped_sequences_become_zero_in_every_layout(dtype, D, layout):
     lens = [(37 * i * i) % 91 for i in range(40)]        # some empty
     run(lens, 6, 2, D, dtype, False, layout, alive=list(range(1, 40, 3)), behind=3)
+
+
+@pytest.mark.parametrize("dtype,D", [(F32, 64), (BF16, 64), (BF16, 128)])
+def test_offsets_beyond_32_bits(dtype, D):
+    """Tokens 2^23 elements apart, 2.5e9 elements from the first to the last: the same bits as side by side."""
+    lens, Hq, Hk, far = [100, 130, 70], 4, 2, 1 << 23
+    starts, total = packed(lens), sum(lens)
+    store = torch.empty(total * far, dtype=dtype, device="cuda")
+    place = [0]
+
+    def apart(h, like=None):
+        x = torch.as_strided(store, (total, h, D), (far, D, 1), place[0])
+        place[0] += h * D
+        return x if like is None else x.copy_(like)
+
+    q, k, v = tensors(total, Hq, Hk, D, dtype, "plain", 5)
+    do = tensors(total, Hq, Hk, D, dtype, "plain", 6)[0]
+    op = vb.Attention(total, 3, Hq, Hk, D, dtype, causal=True)
+    o, lse = op.fwd(q, k, v, starts)
+    kept = dict(alive_in=torch.tensor([1, 2, 0], dtype=torch.int32, device="cuda"), alive_cnt_in=torch.tensor([2], dtype=torch.int32, device="cuda"))
+    want = op.bwd(do, q, k, v, o, lse, starts, **kept)
+    q2, k2, v2, do2 = apart(Hq, q), apart(Hk, k), apart(Hk, v), apart(Hq, do)
+    o2, lse2 = op.fwd(q2, k2, v2, starts, o=apart(Hq))
+    got = op.bwd(do2, q2, k2, v2, o2, lse2, starts, dq=apart(Hq), dk=apart(Hk), dv=apart(Hk), **kept)
+    assert op.device_status() == 0
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)

@@ -280,3 +280,22 @@ def test_refusals():
         op.fwd(torch.zeros(5, 50, device="cuda"), torch.zeros(5, dtype=torch.int64, device="cuda"))
     with pytest.raises(vb.VcasError):
         op.bwd(x, t, v, v, g_entropy=v)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_offsets_beyond_32_bits(dtype):
+    """Rows 2^24 elements apart, 2.3e9 elements from the first to the last: the same bits as side by side."""
+    rows, vocab, far = 140, 1000, 1 << 24
+    x = logits_of(rows, vocab, dtype, pad=8)
+    tokens = tokens_of(rows, vocab)
+    op = vb.TokenLoss(rows, vocab, dtype, top=5)
+    apart = lambda at: torch.as_strided(store, (rows, vocab), (far, 1), at)
+    store = torch.empty(rows * far, dtype=dtype, device="cuda")
+    y = apart(0).copy_(x)
+    a, b = op.fwd(x, tokens), op.fwd(y, tokens)
+    for name in ("logp", "entropy", "lse", "top_logp", "top_ids"):
+        assert torch.equal(getattr(a, name), getattr(b, name)), name
+    g = -torch.rand(rows, device="cuda")
+    want = op.bwd(x, tokens, a.lse, g, entropy=a.entropy, g_entropy=0.1 * g)
+    got = op.bwd(y, tokens, a.lse, g, entropy=a.entropy, g_entropy=0.1 * g, dlogits=apart(4096))
+    assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
