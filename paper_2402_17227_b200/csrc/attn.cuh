@@ -65,6 +65,14 @@ __device__ __forceinline__ int seq_count(const Seqs& q) {
   atomicExch(q.status, (int32_t)VCAS_ERR_BAD_ARG);
   return 0;
 }
+// The k-th sequence to be worked on; -1, and a note, where the list of kept ones does not ascend within 0 .. N - 1.
+__device__ __forceinline__ int seq_listed(const Seqs& q, int k) {
+  if (q.alive == nullptr) return k;
+  const int n = __ldcg(q.alive + k), before = k > 0 ? __ldcg(q.alive + k - 1) : -1;
+  if (n >= 0 && n < q.N && n > before) return n;
+  atomicExch(q.status, (int32_t)VCAS_ERR_BAD_ARG);
+  return -1;
+}
 
 // Tile number `tile` of all sequences cut into tiles of `rows` tokens, sequence by sequence: its sequence's first token and length, and
 // its place in the sequence.  By one full warp, 32 sequences at a time; false where there are not that many tiles.
@@ -72,14 +80,8 @@ __device__ __forceinline__ bool find_tile(const Seqs& q, int tile, int rows, int
   const int count = seq_count(q);
   int before = 0;
   for (int b = 0; b < count; b += 32) {
-    int n = b + lane < count ? b + lane : -1, s = 0, l = 0;
-    if (n >= 0 && q.alive != nullptr) {
-      n = __ldcg(q.alive + n);
-      if (n < 0 || n >= q.N) {
-        atomicExch(q.status, (int32_t)VCAS_ERR_BAD_ARG);
-        n = -1;
-      }
-    }
+    const int n = b + lane < count ? seq_listed(q, b + lane) : -1;
+    int s = 0, l = 0;
     if (n >= 0) l = seq_length(q, n, s);
     const int tiles = (l + rows - 1) / rows;
     int upto = tiles;
@@ -118,9 +120,8 @@ struct Order {
       first[i] = len[i] = 0;
       const int k = 32 * i + lane;
       if (sorted && k < count) {
-        const int n = q.alive != nullptr ? __ldcg(q.alive + k) : k;
-        if (n >= 0 && n < q.N) len[i] = seq_length(q, n, first[i]);
-        else atomicExch(q.status, (int32_t)VCAS_ERR_BAD_ARG);
+        const int n = seq_listed(q, k);
+        if (n >= 0) len[i] = seq_length(q, n, first[i]);
       }
       tiles[i] = (len[i] + 127) / 128;
     }

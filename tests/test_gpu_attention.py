@@ -450,3 +450,25 @@ def test_offsets_beyond_32_bits(dtype, D):
     assert torch.equal(o, o2) and torch.equal(lse, lse2)
     for a, b in zip(want, got):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n", [4, 200])
+def test_a_list_that_does_not_ascend_is_reported(dtype, n):
+    """The same sequence twice: the second entry is left out and reported, the others' results are those of the list without it."""
+    lens = [33 + 7 * (i % 5) for i in range(n)]
+    starts, total = packed(lens), sum(lens)
+    q, k, v = tensors(total, 2, 1, 64, dtype, "plain", 8)
+    do = tensors(total, 2, 1, 64, dtype, "plain", 9)[0]
+    op = vb.Attention(total, n, 2, 1, 64, dtype, causal=True)
+    o, lse = op.fwd(q, k, v, starts)
+    lst = lambda x: dict(alive_in=torch.tensor(x + [0] * (n - len(x)), dtype=torch.int32, device="cuda"),
+                         alive_cnt_in=torch.tensor([len(x)], dtype=torch.int32, device="cuda"))
+    want = op.bwd(do, q, k, v, o, lse, starts, **lst([1, n - 1]))
+    assert op.device_status() == 0
+    got = op.bwd(do, q, k, v, o, lse, starts, **lst([1, 1, n - 1]))
+    assert op.device_status() == -1
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
+    op.bwd(do, q, k, v, o, lse, starts, **lst([n - 1, 1]))
+    assert op.device_status() == -1 and op.device_status() == 0
