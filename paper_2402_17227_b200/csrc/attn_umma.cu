@@ -9,11 +9,11 @@
 //   forward    S = Q K^T,  P = exp(S - m),  O += P V; O is rescaled only where the maximum has risen by more than 2^8
 //   dQ         rows are queries: S, dP = dO V^T, dS = P (dP - delta), dQ += dS K
 //   dK, dV     rows are keys:    S^T = K Q^T, dV += P^T dO, dP^T = V dO^T, dK += dS^T Q, over all query heads of the group
-// P and dS are rounded to bf16, each by up to 2^-9 of itself.  Over many keys these errors are small beside what O and dQ are rounded by
-// themselves; few keys average little.  So the first tile of rows that see FEW keys or less is multiplied as a sum of two bf16 (`few`),
-// with the low parts in the other half of the scores' columns: outputs of such rows are off by their own rounding alone (0.0017 of
-// their norm, 0.0025 by one product).  8 x 2048 tokens, 32/8 heads of 128, causal: forward 267 -> 271 us; backward over 16 sequences of
-// 1 to 2048: 408 -> 411 us.
+// P and dS are rounded to bf16, each by up to 2^-8 of itself: over many keys that makes a result's error 0.0024 of its norm, of which
+// 0.0017 are its own rounding; over few keys single ones show, and more than that.  So the first tile of rows that see FEW keys or less
+// is multiplied as a sum of two bf16 (`few`), with the low parts in the other half of the scores' columns, which leaves such
+// results their own rounding alone; for every tile it would be one product more of two (forward) or five.  8 x 2048 tokens, 32/8
+// heads of 128, causal: forward 267 -> 271 us; backward over 16 sequences of 1 to 2048: 408 -> 411 us.
 // A tile that reaches past its sequence's end holds rows of the next one (or zeros): their scores are masked, and where such rows
 // would be summed over they are zeroed in shared memory, so that nothing of them, a NaN included, gets in.
 #include <type_traits>
