@@ -128,7 +128,8 @@ int vcas_loss_status(vcas_loss l, int32_t* status);
  * consecutive elements (m_scale, v_scale [(n + 255) / 256]); m = value * scale, v = (value * scale)^2.  The step uses the
  * unrounded new m and v; scale = largest of the block / 448, and value / scale goes to one of its two e4m3
  * neighbours, up with the probability of where it lies between them (to 8 random bits), so that a state
- * that moves by less than a rounding step per step still moves; a positive r never becomes 0.  Random bits:
+ * that moves by less than a rounding step per step still moves; a positive r never becomes 0, and an infinite one (a finite g'
+ * whose square is not: p then only decays in this step, by the formula) is held as 2^63.  Random bits:
  * Philox4x32-10 with key = (seed low, seed high), counter = (element / 8, tensor's place in the list, 3, 0); of element e,
  * word e % 8 / 2, halfword e % 2: low byte for m, high byte for r.  Give another seed each step.
  * A NaN or infinite gradient spoils its element, and with 8-bit states the states of its block.

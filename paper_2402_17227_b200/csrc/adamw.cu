@@ -157,19 +157,28 @@ __device__ __forceinline__ Eight decode(uint2 c, float scale) {
 }
 // A value times 2^-120 has its e4m3 exponent and mantissa in bits 20-26, subnormals included; what is below them decides together with the
 // random bits (in bits 12-19, and half of their step) whether the code goes up by one.  BYTE: of each element's halfword.
-// POSITIVE: no signs, and a positive value does not become 0.  A value may come out up to 3 steps of fp32 above 448, too few to
-// reach the next code: what is added is at most 2^20 - 2048.
+// POSITIVE: no signs, a positive value does not become 0, and an infinite one (a finite gradient whose square is not) is held as 2^63:
+// as infinity it would take the scale, and with it the block's other states, along.  A value may come out up to 3 steps of fp32
+// above 448, too few to reach the next code: what is added is at most 2^20 - 2048.
 __device__ __forceinline__ uint32_t largest(uint32_t top, float a, float b) {
   float r;
   asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(__uint_as_float(top)), "f"(a), "f"(b));
   return __float_as_uint(r);
 }
-template <bool POSITIVE, int BYTE>
-__device__ __forceinline__ uint2 encode(const float (&f)[8], const uint32_t (&rnd)[4], float* scale_at, int lane) {
+__device__ __forceinline__ float largest_of_block(const float (&f)[8]) {
   uint32_t top = 0;
 #pragma unroll
   for (int i = 0; i < 8; i += 2) top = largest(top, f[i], f[i + 1]);
-  const float big = __uint_as_float(__reduce_max_sync(0xffffffffu, top));
+  return __uint_as_float(__reduce_max_sync(0xffffffffu, top));
+}
+template <bool POSITIVE, int BYTE>
+__device__ __forceinline__ uint2 encode(float (&f)[8], const uint32_t (&rnd)[4], float* scale_at, int lane) {
+  float big = largest_of_block(f);
+  if (POSITIVE && big == __int_as_float(0x7f800000)) {       // the same in all lanes
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = f[i] == __int_as_float(0x7f800000) ? 0x1p63f : f[i];
+    big = largest_of_block(f);
+  }
   if (lane == 0) *scale_at = __fmul_rn(big, 1.0f / 448.0f);
   // under 2^-100 (sqrt(v) is never that small) 1 / big would leave fp32's range: such an m is held as 0
   const float inv = big >= 0x1p-100f ? __fmul_rn(__frcp_rn(big), 448.0f) : 0.f;
@@ -190,14 +199,14 @@ __device__ __forceinline__ uint2 encode(const float (&f)[8], const uint32_t (&rn
 }
 
 // sqrt(x), rounded correctly but for the rarest x: x / sqrt(x) and one step of Newton's iteration on its exact residual.  x under fp32's
-// normal numbers counts as the least of them: the approximation would take it for 0.
+// normal numbers counts as the least of them: the approximation would take it for 0.  The minimum with x 2^126, which is above
+// the root of any other number, gives 0 its root, and infinity, of whose root the iteration makes a NaN; a NaN stays one.
 __device__ __forceinline__ float root_of(float x) {
-  const float y = fmaxf(x, 0x1p-126f);
-  float r;
+  float y, r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(x), "f"(0x1p-126f));
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(y));
   const float s = __fmul_rn(y, r);
-  const float better = fmaf(fmaf(-s, s, y), 0.5f * r, s);
-  return x > 0.f ? better : x;           // 0, and what is no number
+  return fminf(fmaf(fmaf(-s, s, y), 0.5f * r, s), __fmul_rn(x, 0x1p126f));
 }
 // 1 / x, good to an ulp, of a normal x
 __device__ __forceinline__ float reciprocal(float x) {
