@@ -32,7 +32,9 @@ extern "C" {
  * are rounded to bf16 where they enter a product (on the tensor cores to a sum of two bf16 where a sequence's first rows, of
  * 64 keys or less, are concerned), O and the gradients once when stored.
  * A sequence may be empty.  Rows from starts[N] on are neither read nor written.  starts that descend, are negative
- * or pass `total` are not followed: those sequences are left out and vcas_attn_status reports VCAS_ERR_BAD_ARG.
+ * or pass `total` are not followed: those sequences are left out (nothing is written to their rows) and vcas_attn_status
+ * reports VCAS_ERR_BAD_ARG.  The results of sequences that such starts make overlap, and of those listed behind them, are unspecified,
+ * and rows of sequences that a backward drops may then be left unwritten.
  * A NaN or infinity in a row of q, k or v reaches that sequence's results only.
  */
 typedef struct vcas_attn_s* vcas_attn;

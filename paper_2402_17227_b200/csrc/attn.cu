@@ -217,6 +217,22 @@ __device__ __forceinline__ void p_and_ds(const AttnCall& C, const Place& p, int 
       dp[i][j] = see && !alone ? s[i][j] * (dp[i][j] - delta[i]) : 0.f;
     }
 }
+// rowsum(dO O) of this thread's rows, from tiles of both; every thread of a row has it
+template <int DP>
+__device__ __forceinline__ void row_sums(const float* a, const float* b, int tx, int ty, float (&sum)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    sum[i] = 0.f;
+#pragma unroll
+    for (int jj = 0; jj < DP / 64; ++jj) {
+      const int at = (ty * 4 + i) * (DP + 4) + tx * 4 + 64 * jj;
+      const float4 x = *reinterpret_cast<const float4*>(a + at), y = *reinterpret_cast<const float4*>(b + at);
+      sum[i] = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, sum[i]))));
+    }
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
+  }
+}
 // lse in units of log 2, and delta, of this thread's rows
 __device__ __forceinline__ void row_values(const AttnCall& C, const Place& p, int i0, int head, int ty, float (&lse)[4], float (&delta)[4]) {
 #pragma unroll
@@ -237,8 +253,17 @@ __global__ void __launch_bounds__(THREADS) attn_fma_dq_kernel(AttnCall C) {
   if (!p.any) return;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   load_two<T, DP>(sq, C.q, sdo, C.d_o, p.first, p.len, p.t0, p.head, C.dim);
+  load_tile<T, DP>(sk, C.o, p.first, p.len, p.t0, p.head, C.dim);
   float lse[4], delta[4], acc[4][DP / 16];
-  row_values(C, p, p.t0, p.head, ty, lse, delta);
+  __syncthreads();
+  row_sums<DP>(sdo, sk, tx, ty, delta);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int t = p.t0 + ty * 4 + i;
+    const int64_t at = (int64_t)p.head * C.seqs.total + p.first + t;
+    lse[i] = t < p.len ? C.lse[at] * ATTN_LOG2E : 0.f;
+    if (tx == 0 && t < p.len) C.delta[at] = delta[i];        // for the dK, dV kernel
+  }
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -315,21 +340,39 @@ __global__ void __launch_bounds__(THREADS) attn_fma_dkv_kernel(AttnCall C) {
   store_rows<T, DP>(C.dk, p.first, p.len, p.t0, p.head, C.dim, tx, ty, dk, f);
 }
 
-// A warp for some tokens one behind the other: delta of their heads where the sequence is worked on (DELTA), else zeros in their rows of the
-// gradients.  wide: those rows can be written 16 bytes at a time.
-template <typename T, bool DELTA>
-__global__ void __launch_bounds__(256, 8) attn_rows_kernel(AttnCall C, bool wide) {
+// Zeros in the gradients' rows of the sequences that are not worked on.  A warp has some tokens one behind the other, and finds their
+// sequences and whether these are kept by bisection.  wide: rows can be written 16 bytes at a time.
+template <typename T>
+__global__ void __launch_bounds__(128, 16) attn_zero_kernel(AttnCall C, bool wide) {
   pdl_trigger();                         // what follows works on other sequences
   const Seqs& q = C.seqs;
   const int lane = threadIdx.x & 31, in_cta = (int)(blockDim.x >> 5), warps = (int)gridDim.x * in_cta;
-  const int each = (q.total + warps - 1) / warps;
-  const int64_t from = (int64_t)((int)blockIdx.x * in_cta + (int)(threadIdx.x >> 5)) * each;
-  const int to = (int)min((int64_t)q.total, from + each);
+  const int warp = (int)blockIdx.x * in_cta + (int)(threadIdx.x >> 5);
+  const int count = seq_count(q);
   // a row of zeros in pieces of 16 bytes: this lane's piece of a head, and its heads mine, mine + at_once, ...
   constexpr int VN = 16 / sizeof(T);
   const int per = C.dim / VN, at_once = 32 / per, piece = lane % per, mine = lane / per < at_once ? lane / per : 1 << 20;
+  auto zero_row = [&](int t) {
+    auto zero = [&](const Strided& x, int heads) {
+      T* base = (T*)const_cast<void*>(x.p) + (int64_t)t * x.token;
+      if (wide) {
+        base += mine * x.head + piece * VN;
+        const int64_t step = at_once * x.head;
+#pragma unroll 4
+        for (int h = mine; h < heads; h += at_once, base += step) *reinterpret_cast<uint4*>(base) = make_uint4(0, 0, 0, 0);
+      } else {
+        for (int i = lane; i < heads * C.dim; i += 32) put(base + (int64_t)(i / C.dim) * x.head + i % C.dim, 0.f);
+      }
+    };
+    zero(C.dq, C.heads_q);
+    zero(C.dk, C.heads_kv);
+    zero(C.dv, C.heads_kv);
+  };
+  const int each = (q.total + warps - 1) / warps;
+  const int64_t from = (int64_t)warp * each;
+  const int to = (int)min((int64_t)q.total, from + each);
   int first = 0, end = 0;                // the sequence that t lies in, once found
-  bool alive = true;
+  bool kept = false;
   for (int t = (int)min((int64_t)q.total, from); t < to; ++t) {
     if (t < first || t >= end) {
       // the last sequence that begins at or before t (the empty ones before it begin there too)
@@ -341,45 +384,15 @@ __global__ void __launch_bounds__(256, 8) attn_rows_kernel(AttnCall C, bool wide
       const int len = seq_length(q, lo, first);
       end = first + len;
       if (t < first || t >= end) continue;
-      if (q.alive != nullptr) {
-        int a = 0, b = seq_count(q);
-        const int count = b;
-        while (a < b) {
-          const int mid = (a + b) >> 1;
-          if (q.alive[mid] < lo) a = mid + 1; else b = mid;
-        }
-        alive = a < count && q.alive[a] == lo;
+      int a = 0, b = count;
+      while (a < b) {
+        const int mid = (a + b) >> 1;
+        if (q.alive[mid] < lo) a = mid + 1; else b = mid;
       }
+      kept = a < count && q.alive[a] == lo;
     }
-    if (alive) {
-      if (!DELTA) {
-        t = end - 1;                     // nothing to do up to there
-        continue;
-      }
-      for (int h = 0; h < C.heads_q; ++h) {
-        const T* o = (const T*)C.o.p + (int64_t)t * C.o.token + (int64_t)h * C.o.head;
-        const T* g = (const T*)C.d_o.p + (int64_t)t * C.d_o.token + (int64_t)h * C.d_o.head;
-        float s = 0.f;
-        for (int d = lane; d < C.dim; d += 32) s = fmaf(widen(o[d]), widen(g[d]), s);
-        s = warp_sum(s);
-        if (lane == 0) C.delta[(int64_t)h * q.total + t] = s;
-      }
-    } else if (!C.skip_dropped) {
-      auto zero = [&](const Strided& x, int heads) {
-        T* base = (T*)const_cast<void*>(x.p) + (int64_t)t * x.token;
-        if (wide) {
-          base += mine * x.head + piece * VN;
-          const int64_t step = at_once * x.head;
-#pragma unroll 4
-          for (int h = mine; h < heads; h += at_once, base += step) *reinterpret_cast<uint4*>(base) = make_uint4(0, 0, 0, 0);
-        } else {
-          for (int i = lane; i < heads * C.dim; i += 32) put(base + (int64_t)(i / C.dim) * x.head + i % C.dim, 0.f);
-        }
-      };
-      zero(C.dq, C.heads_q);
-      zero(C.dk, C.heads_kv);
-      zero(C.dv, C.heads_kv);
-    }
+    if (kept) t = end - 1;               // nothing to do up to there
+    else zero_row(t);
   }
 }
 
@@ -450,8 +463,8 @@ cudaError_t attn_fma_prepare() {
   if (e == cudaSuccess) e = room<__nv_bfloat16, 128>();
   // an SM divides its memory anew only when it is idle: as the kernel needs it that is to begin beside this one
   auto beside = [](const void* k) { return cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared); };
-  if (e == cudaSuccess) e = beside((const void*)attn_rows_kernel<float, false>);
-  if (e == cudaSuccess) e = beside((const void*)attn_rows_kernel<__nv_bfloat16, false>);
+  if (e == cudaSuccess) e = beside((const void*)attn_zero_kernel<float>);
+  if (e == cudaSuccess) e = beside((const void*)attn_zero_kernel<__nv_bfloat16>);
   return e;
 }
 cudaError_t launch_attn_fma_fwd(const Attn* a, const AttnCall& c, cudaStream_t st) {
@@ -459,28 +472,27 @@ cudaError_t launch_attn_fma_fwd(const Attn* a, const AttnCall& c, cudaStream_t s
     return c.dim <= 64 ? fwd<__nv_bfloat16, 64>(c, st) : fwd<__nv_bfloat16, 128>(c, st);
   return c.dim <= 64 ? fwd<float, 64>(c, st) : fwd<float, 128>(c, st);
 }
-template <bool DELTA>
-static cudaError_t rows(const Attn* a, const AttnCall& c, cudaStream_t st) {
-  // delta: a warp a token.  Zeros alone are written beside the kernel that follows: one small CTA an SM leaves it its registers, and as
-  // all of them begin at once, so does that kernel (64 x 197 tokens of 12 heads of 64, 40 % kept:
-  // 57.7 us for the whole backward, 64.8 with a warp a token).
-  const int threads = DELTA ? 256 : 128, most = (c.seqs.total + threads / 32 - 1) / (threads / 32);
-  const unsigned grid = (unsigned)(DELTA ? most : (most < a->num_sms ? most : a->num_sms));
-  const int elem = a->desc.dtype == VCAS_DTYPE_BF16 ? 2 : 4, vn = 16 / elem;
-  auto wide = [&](const Strided& x) { return ((uintptr_t)x.p & 15) == 0 && x.token % vn == 0 && x.head % vn == 0; };
-  const bool w = wide(c.dq) && wide(c.dk) && wide(c.dv);
-  if (elem == 2) attn_rows_kernel<__nv_bfloat16, DELTA><<<grid, threads, 0, st>>>(c, w);
-  else attn_rows_kernel<float, DELTA><<<grid, threads, 0, st>>>(c, w);
-  return cudaGetLastError();
-}
 cudaError_t launch_attn_fma_bwd(const Attn* a, const AttnCall& c, cudaStream_t st) {
-  const cudaError_t e = rows<true>(a, c, st);
-  if (e != cudaSuccess) return e;
+  if (c.seqs.alive != nullptr && !c.skip_dropped) {
+    const cudaError_t e = launch_attn_zero(a, c, st);
+    if (e != cudaSuccess) return e;
+  }
   if (a->desc.dtype == VCAS_DTYPE_BF16)
     return c.dim <= 64 ? bwd<__nv_bfloat16, 64>(c, st) : bwd<__nv_bfloat16, 128>(c, st);
   return c.dim <= 64 ? bwd<float, 64>(c, st) : bwd<float, 128>(c, st);
 }
-cudaError_t launch_attn_zero(const Attn* a, const AttnCall& c, cudaStream_t st) { return rows<false>(a, c, st); }
+cudaError_t launch_attn_zero(const Attn* a, const AttnCall& c, cudaStream_t st) {
+  // Beside the kernel that follows: one small CTA an SM leaves it its registers, and as all of them begin at once, so does that kernel
+  // (64 x 197 tokens of 12 heads of 64, 40 % kept: 57.7 us for the whole backward, 64.8 with a warp a token).
+  const int threads = 128, most = (c.seqs.total + threads / 32 - 1) / (threads / 32);
+  const unsigned grid = (unsigned)(most < a->num_sms ? most : a->num_sms);
+  const int elem = a->desc.dtype == VCAS_DTYPE_BF16 ? 2 : 4, vn = 16 / elem;
+  auto wide = [&](const Strided& x) { return ((uintptr_t)x.p & 15) == 0 && x.token % vn == 0 && x.head % vn == 0; };
+  const bool w = wide(c.dq) && wide(c.dk) && wide(c.dv);
+  if (elem == 2) attn_zero_kernel<__nv_bfloat16><<<grid, threads, 0, st>>>(c, w);
+  else attn_zero_kernel<float><<<grid, threads, 0, st>>>(c, w);
+  return cudaGetLastError();
+}
 
 }  // namespace vcas
 
