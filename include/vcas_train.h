@@ -70,8 +70,8 @@ int vcas_attn_fwd(vcas_attn a, const vcas_attn_tensor* q, const vcas_attn_tensor
  * ascending list of the sequences whose rows of d_o may be non-zero, as vcas_linear_bwd_chain's kept_out gives it for the
  * layer above (Sec. 4: data dropped by SampleA have a zero gradient in every layer below).  The others are not
  * computed and none of their rows is read; their rows of dq, dk, dv are set to zero, or, with skip_dropped_rows,
- * left unwritten.  A length outside [0, N], an entry outside [0, N) or one that is not above the entry before it is not
- * followed and reported like bad starts.
+ * left unwritten.  A length outside [0, N] (the list then counts as empty), an entry outside [0, N) and one that is not above
+ * all others before it are not followed and reported like bad starts.
  */
 int vcas_attn_bwd(vcas_attn a, const vcas_attn_tensor* d_o, const vcas_attn_tensor* q, const vcas_attn_tensor* k,
                   const vcas_attn_tensor* v, const vcas_attn_tensor* o, const float* lse, const int32_t* starts, int32_t N,

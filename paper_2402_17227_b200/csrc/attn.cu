@@ -341,7 +341,8 @@ __global__ void __launch_bounds__(THREADS) attn_fma_dkv_kernel(AttnCall C) {
 }
 
 // Zeros in the gradients' rows of the sequences that are not worked on.  A warp has some tokens one behind the other, and finds their
-// sequences and whether these are kept by bisection.  wide: rows can be written 16 bytes at a time.
+// sequences by bisection.  Whether these are kept it reads from the list, as it goes through it once; a long one that ascends is
+// searched by bisection too.  wide: rows can be written 16 bytes at a time.
 template <typename T>
 __global__ void __launch_bounds__(128, 16) attn_zero_kernel(AttnCall C, bool wide) {
   pdl_trigger();                         // what follows works on other sequences
@@ -349,6 +350,16 @@ __global__ void __launch_bounds__(128, 16) attn_zero_kernel(AttnCall C, bool wid
   const int lane = threadIdx.x & 31, in_cta = (int)(blockDim.x >> 5), warps = (int)gridDim.x * in_cta;
   const int warp = (int)blockIdx.x * in_cta + (int)(threadIdx.x >> 5);
   const int count = seq_count(q);
+  bool in_order = false;
+  if (count > 256) {
+    int good = 1;
+#pragma unroll 4
+    for (int k = threadIdx.x; k < count; k += 128) {
+      const int n = __ldcg(q.alive + k), before = k > 0 ? __ldcg(q.alive + k - 1) : -1;
+      good &= n < q.N && n > before;
+    }
+    in_order = __syncthreads_and(good);
+  }
   // a row of zeros in pieces of 16 bytes: this lane's piece of a head, and its heads mine, mine + at_once, ...
   constexpr int VN = 16 / sizeof(T);
   const int per = C.dim / VN, at_once = 32 / per, piece = lane % per, mine = lane / per < at_once ? lane / per : 1 << 20;
@@ -368,6 +379,25 @@ __global__ void __launch_bounds__(128, 16) attn_zero_kernel(AttnCall C, bool wid
     zero(C.dk, C.heads_kv);
     zero(C.dv, C.heads_kv);
   };
+  // The entries that count (see seq_listed) ascend, and the first that is n or more is one of them.  at: where in the list it may be; a
+  // later sequence's is not before it.
+  int at = 0;
+  auto is_kept = [&](int n) {
+    if (in_order) {
+      int a = 0, b = count;
+      while (a < b) {
+        const int mid = (a + b) >> 1;
+        if (q.alive[mid] < n) a = mid + 1; else b = mid;
+      }
+      return a < count && q.alive[a] == n;
+    }
+    for (; at < count; at += 32) {
+      const int v = at + lane < count ? __ldcg(q.alive + at + lane) : -1;
+      const unsigned hit = __ballot_sync(0xffffffffu, v >= n && v < q.N);
+      if (hit != 0) return __shfl_sync(0xffffffffu, v, __ffs(hit) - 1) == n;
+    }
+    return false;
+  };
   const int each = (q.total + warps - 1) / warps;
   const int64_t from = (int64_t)warp * each;
   const int to = (int)min((int64_t)q.total, from + each);
@@ -384,12 +414,7 @@ __global__ void __launch_bounds__(128, 16) attn_zero_kernel(AttnCall C, bool wid
       const int len = seq_length(q, lo, first);
       end = first + len;
       if (t < first || t >= end) continue;
-      int a = 0, b = count;
-      while (a < b) {
-        const int mid = (a + b) >> 1;
-        if (q.alive[mid] < lo) a = mid + 1; else b = mid;
-      }
-      kept = a < count && q.alive[a] == lo;
+      kept = is_kept(lo);
     }
     if (kept) t = end - 1;               // nothing to do up to there
     else zero_row(t);

@@ -48,11 +48,12 @@ __device__ __forceinline__ float attn_exp2(float x) {
   return y;
 }
 
+__device__ __forceinline__ bool seq_sane(const Seqs& q, int s, int e) { return s >= 0 && e >= s && e <= q.total; }
 // Sequence n: its first token and length; 0 tokens and a note in the status word where starts make no sense there.
 __device__ __forceinline__ int seq_length(const Seqs& q, int n, int& first) {
   const int s = __ldcg(q.starts + n), e = __ldcg(q.starts + n + 1);   // past L1: a kernel may begin beside the one before it
   first = s;
-  if (s < 0 || e < s || e > q.total) {
+  if (!seq_sane(q, s, e)) {
     atomicExch(q.status, (int32_t)VCAS_ERR_BAD_ARG);
     return 0;
   }
@@ -65,22 +66,41 @@ __device__ __forceinline__ int seq_count(const Seqs& q) {
   atomicExch(q.status, (int32_t)VCAS_ERR_BAD_ARG);
   return 0;
 }
-// The k-th sequence to be worked on; -1, and a note, where the list of kept ones does not ascend within 0 .. N - 1.
-__device__ __forceinline__ int seq_listed(const Seqs& q, int k) {
-  if (q.alive == nullptr) return k;
-  const int n = __ldcg(q.alive + k), before = k > 0 ? __ldcg(q.alive + k - 1) : -1;
-  if (n >= 0 && n < q.N && n > before) return n;
-  atomicExch(q.status, (int32_t)VCAS_ERR_BAD_ARG);
-  return -1;
+// Entries of the list of sequences to be worked on count while they are in 0 .. N - 1 and above all entries before them.
+// The part of seq_listed for lists that are not in order.  top: the largest entry so far, or -2 where all up to this block ascend.
+// Returns the entry, or -1 where it does not count, and the new top.
+__device__ __noinline__ inline int2 seq_listed_anyhow(int raw, int before, bool there, int N, int top, int lane, int32_t* status) {
+  if (top == -2) top = __shfl_sync(0xffffffffu, before, 0);
+  const bool in = there && raw >= 0 && raw < N;
+  int below = __shfl_up_sync(0xffffffffu, in ? raw : -1, 1);
+  below = lane == 0 ? top : max(below, top);
+#pragma unroll 1
+  for (int o = 1; o < 32; o <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, below, o);
+    if (lane >= o) below = max(below, v);
+  }
+  if (there && !(in && raw > below)) atomicExch(status, (int32_t)VCAS_ERR_BAD_ARG);
+  return make_int2(in && raw > below ? raw : -1, max(top, __reduce_max_sync(0xffffffffu, in ? raw : -1)));
+}
+// Entry k of the list, a lane's own of 32 one behind the other, by a full warp that goes through the list from its beginning (top: -2
+// there); -1 behind its end and, with a note, where it does not count.
+__device__ __forceinline__ int seq_listed(const Seqs& q, int k, int count, int lane, int& top) {
+  const bool there = k < count;
+  if (q.alive == nullptr) return there ? k : -1;
+  const int n = there ? __ldcg(q.alive + k) : -1, before = there && k > 0 ? __ldcg(q.alive + k - 1) : -1;
+  if (top == -2 && __all_sync(0xffffffffu, (n < q.N && n > before) || !there)) return n;
+  const int2 r = seq_listed_anyhow(n, before, there, q.N, top, lane, q.status);
+  top = r.y;
+  return r.x;
 }
 
 // Tile number `tile` of all sequences cut into tiles of `rows` tokens, sequence by sequence: its sequence's first token and length, and
 // its place in the sequence.  By one full warp, 32 sequences at a time; false where there are not that many tiles.
 __device__ __forceinline__ bool find_tile(const Seqs& q, int tile, int rows, int lane, int& first, int& len, int& place) {
   const int count = seq_count(q);
-  int before = 0;
+  int before = 0, top = -2;
   for (int b = 0; b < count; b += 32) {
-    const int n = b + lane < count ? seq_listed(q, b + lane) : -1;
+    const int n = seq_listed(q, b + lane, count, lane, top);
     int s = 0, l = 0;
     if (n >= 0) l = seq_length(q, n, s);
     const int tiles = (l + rows - 1) / rows;
@@ -115,16 +135,18 @@ struct Order {
   __device__ __forceinline__ Order(const Seqs& q, int lane, bool causal_, bool keys_) : causal(causal_), keys(keys_) {
     const int count = seq_count(q);
     sorted = count <= 32 * SLOTS;
+    bool astray = false;                 // lists that are not in order: as find_tile goes through them
 #pragma unroll
     for (int i = 0; i < SLOTS; ++i) {
       first[i] = len[i] = 0;
       const int k = 32 * i + lane;
       if (sorted && k < count) {
-        const int n = seq_listed(q, k);
-        if (n >= 0) len[i] = seq_length(q, n, first[i]);
+        const int n = q.alive == nullptr ? k : __ldcg(q.alive + k), before = q.alive == nullptr || k == 0 ? -1 : __ldcg(q.alive + k - 1);
+        if (n < q.N && n > before) len[i] = seq_length(q, n, first[i]); else astray = true;
       }
       tiles[i] = (len[i] + 127) / 128;
     }
+    if (__any_sync(0xffffffffu, astray)) sorted = false;
     // sequences of one length: in their order, whose tiles share more in L2 (8 x 2048 tokens forward: 283 us, sorted 291)
     int most = 0, least = 1 << 30;
 #pragma unroll
@@ -178,8 +200,9 @@ struct Order {
   }
 };
 
-// No more tiles than these exist where sequences do not overlap: a sequence adds one that is not full at most.
-inline long tile_bound(int total, int N, int rows) { return total / rows + (N < total ? N : total); }
+// No more tiles than these exist where sequences do not overlap: a sequence adds one that is not full at most.  If one is left out, or
+// there are more than tokens, one tile is not found, and looking for it sees every sequence (what is wrong with any is noted).
+inline long tile_bound(int total, int N, int rows) { return total / rows + (N < total ? N : total + 1); }
 
 cudaError_t attn_fma_prepare();
 cudaError_t launch_attn_fma_fwd(const Attn* a, const AttnCall& c, cudaStream_t st);

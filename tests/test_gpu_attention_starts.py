@@ -65,3 +65,11 @@ def run(dtype, layout, D, case, kept):
 @pytest.mark.parametrize("case", range(len(CASES)))
 def test_other_sequences_keep_their_results(dtype, layout, D, case):
     run(dtype, layout, D, case, None)
+
+
+@pytest.mark.parametrize("dtype,layout", [(F32, "plain"), (F32, "odd"), (BF16, "plain"), (BF16, "odd")])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("case", range(len(CASES)))
+@pytest.mark.parametrize("kept", [0, 1])
+def test_a_kept_one_keeps_its_results(dtype, layout, D, case, kept):
+    run(dtype, layout, D, case, kept)
