@@ -108,7 +108,8 @@ int vcas_loss_destroy(vcas_loss l);
 int vcas_loss_fwd(vcas_loss l, const void* logits, int64_t ld, const void* tokens, int32_t token_bytes, int32_t rows,
                   float* logp, float* entropy, float* lse, float* top_logp, int32_t* top_ids, vcas_stream stream);
 /*
- * dlogits_j = g_logp (1[j = t] - p_j) - g_entropy p_j (log p_j + entropy) from the forward's lse and entropy;
+ * dlogits_j = g_logp (1[j = t] - p_j) - g_entropy p_j (log p_j + entropy) from the forward's lse and entropy (where lse is 1024 or
+ * more away from 0, its fp32 value is too coarse for p, which then comes from the row's logits alone);
  * g_logp, g_entropy [rows]: the loss's derivatives (g_entropy may be NULL, then entropy may be too).  Rows whose factors
  * are both zero (no token and no entropy term, or g_logp = 0) get zeros and are not read.  dlogits may be logits
  * themselves (same ld).  a_out [rows], may be NULL: the square-norm of every row of dlogits as stored, which

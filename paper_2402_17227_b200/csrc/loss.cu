@@ -504,6 +504,41 @@ struct BwdParams {
   float4* part; int32_t* tickets; int32_t* status;
 };
 
+// x - lse is good to 2^-25 |lse|, and p to as much relative to itself: 2^-15 here, where bf16's own rounding is 2^-9.  Rows farther from 0
+// have their log probabilities from the logits again (with lse, a row throughout at the type's lowest value would have p = 1).
+constexpr float LSE_FAR = 1024.0f;
+
+// Such a row, by a whole CTA: the largest logit, log sum exp(x - it), then the gradient.  All of it is read before any is written, for the
+// two may be the same.  Returns this thread's sum of squares.
+template <typename T, int NT>
+__device__ __noinline__ float far_row(const T* row, T* out, int V, int64_t t, float gl, float nge, float base, float* s_sum) {
+  auto joined = [&](float x, auto join) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x = join(x, __shfl_xor_sync(0xffffffffu, x, o));
+    __syncthreads();                     // what was there before has been read
+    if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x / 32] = x;
+    __syncthreads();
+    x = s_sum[0];
+#pragma unroll
+    for (int w = 1; w < NT / 32; ++w) x = join(x, s_sum[w]);
+    return x;
+  };
+  float m = __int_as_float(0xff800000), s = 0.f, sq = 0.f;
+  for (int i = threadIdx.x; i < V; i += NT) m = fmaxf(m, Vec<T>::one(row[i]));
+  m = joined(m, [](float a, float b) { return fmaxf(a, b); });
+  for (int i = threadIdx.x; i < V; i += NT) s += exp2_fast(max_nan(Vec<T>::one(row[i]) - m, FAR) * LOG2E);
+  const float log_s = logf(joined(s, [](float a, float b) { return a + b; }));
+  for (int i = threadIdx.x; i < V; i += NT) {
+    const float lp = max_nan((Vec<T>::one(row[i]) - m) - log_s, FAR);
+    float d = exp2_fast(lp * LOG2E) * fmaf(nge, lp, base);
+    if (i == t) d += gl;
+    d = Vec<T>::put(d, out + i);
+    sq = fmaf(d, d, sq);
+  }
+  __syncthreads();                       // s_sum is free again
+  return sq;
+}
+
 // dx_j = g_logp (1[j = t] - p_j) - g_entropy p_j (log p_j + entropy): one read and one write of HBM.  The row's square-norm is
 // summed over the stored values on the way.
 template <typename T, int NT>
@@ -515,7 +550,7 @@ __global__ void __launch_bounds__(NT) loss_bwd_kernel(BwdParams P) {
   const int slice = blockIdx.x - (int)r * P.slices;
   const T* row = (const T*)P.x + r * P.ld;
   T* out = (T*)P.dx + r * P.ld_d;
-  const int c0 = slice * P.per, c1 = min(P.V, c0 + P.per);
+  int c0 = slice * P.per, c1 = min(P.V, c0 + P.per);
   int64_t t = token_of(P.tokens, P.token_bytes, r);
   if (t >= P.V) {
     t = -1;
@@ -532,6 +567,11 @@ __global__ void __launch_bounds__(NT) loss_bwd_kernel(BwdParams P) {
     return exp2_fast(lp * LOG2E) * fmaf(nge, lp, base);
   };
   float sq = 0.f;
+  if (fabsf(lse) >= LSE_FAR && !zero) {
+    // by the row's first CTA; the others have nothing to do with it
+    if (slice == 0) sq = far_row<T, NT>(row, out, P.V, t, gl, nge, base, s_sum);
+    c0 = c1 = 0;
+  }
   auto single = [&](int i) {
     float d = zero ? 0.f : value(Vec<T>::one(row[i]));
     if (i == t && !zero) d += gl;
