@@ -781,7 +781,8 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
       if (DC == 2) {
         ok = warp_wait(&s.taken, n & 1, ab, status);
         if (!ok) break;
-        delta = s_half[in] + s_half[128 + in];
+        // with a single tile of keys delta is rowsum(P dP), whose parts another warp may already be writing there
+        if (tiles > 1) delta = s_half[in] + s_half[128 + in];
       }
       const float nl = -lse * ATTN_LOG2E;
       const uint64_t n2 = pack2(nl, nl);
