@@ -51,6 +51,8 @@ class AttentionInput:
 class StackLayer:
     """One linear layer of the stack, in backward order.
 
+    dY: the incoming gradients that a layer is given, and on which it is probed.  One that gets its gradient from the layer above or
+    from a loss needs none: it is then probed on the exact gradients of the batch variants.
     chained: this layer's dY is the dX of the layer before it in backward order.
     attention: this layer's dY is the gradient of an attention whose output is the input of the layer before it in backward
     order.
@@ -62,7 +64,7 @@ class StackLayer:
     d_out: int
     W: torch.Tensor
     X: list            # input activations, one tensor per batch variant [R, d_in]
-    dY: list           # incoming gradients per batch variant [R, d_out] (unused when chained)
+    dY: list           # incoming gradients per batch variant [R, d_out]
     H: list | None = None      # pre-activation of the GELU feeding this layer's input, per variant [R, d_in]
     chained: bool = False
     attention: AttentionInput | None = None
@@ -141,7 +143,7 @@ class LinearStack:
                 dY = prev.dX
                 kw.update(a_in=prev.a_out, a_in_parts=prev.handle.chain_parts())
             elif L.attention is not None:
-                dY = self._attention_grad(L, prev, v, alive_in=prev.kept, alive_cnt_in=prev.kept_cnt,
+                dY = self._attention_grad(L, prev.dX, v, alive_in=prev.kept, alive_cnt_in=prev.kept_cnt,
                                           skip_dropped_rows=self.skip_dropped_rows)
             elif L.loss is not None:
                 dY = self._loss_grad(L, v)
@@ -159,20 +161,20 @@ class LinearStack:
             for h in self.handles.values():
                 h.join()
 
-    def _attention_grad(self, L: StackLayer, prev: StackLayer, v: int, **kept):
+    def _attention_grad(self, L: StackLayer, dO: torch.Tensor, v: int, out=None, **kept):
         """dY of the layer under an attention from the dX of the layer above it; of the kept data only, where they are given."""
-        a = L.attention
+        a, out = L.attention, L.grad if out is None else out
         q, k, vv = a.split(a.qkv[v])
-        dq, dk, dv = a.split(L.grad.view(self.R, -1, a.op.head_dim))
-        a.op.bwd(prev.dX.view(a.o[v].shape), q, k, vv, a.o[v], a.lse[v], a.starts, dq=dq, dk=dk, dv=dv, **kept)
-        return L.grad
+        dq, dk, dv = a.split(out.view(self.R, -1, a.op.head_dim))
+        a.op.bwd(dO.view(a.o[v].shape), q, k, vv, a.o[v], a.lse[v], a.starts, dq=dq, dk=dk, dv=dv, **kept)
+        return out
 
-    def _loss_grad(self, L: StackLayer, v: int):
+    def _loss_grad(self, L: StackLayer, v: int, out=None, norms=None):
         """dY of the top layer, and its rows' square-norms."""
-        o = L.loss
+        o, out = L.loss, L.grad if out is None else out
         o.op.bwd(o.logits[v], o.tokens[v], o.lse[v], o.g_logp[v], entropy=o.entropy[v] if o.entropy else None,
-                 g_entropy=o.g_entropy[v] if o.g_entropy else None, dlogits=L.grad[:, :o.op.vocab], a_out=L.norms)
-        return L.grad
+                 g_entropy=o.g_entropy[v] if o.g_entropy else None, dlogits=out[:, :o.op.vocab], a_out=L.norms if norms is None else norms)
+        return out
 
     def make_optimizer(self, bits: int = 32, weight_decay: float = 0.0) -> vb.AdamW:
         """AdamW over the stack's weights from their dW, in one launch: fp32 weights in place; bf16 ones from fp32 masters that the
@@ -193,7 +195,7 @@ class LinearStack:
             if hook is not None:
                 hook(i, L, False)
             if L.attention is not None:
-                dY = self._attention_grad(L, prev, v)
+                dY = self._attention_grad(L, prev.dX, v)
             elif L.loss is not None:
                 dY = self._loss_grad(L, v)
             else:
@@ -204,14 +206,42 @@ class LinearStack:
                 hook(i, L, True)
             prev = L
 
+    def _exact_grads(self) -> list:
+        """Every layer's dY in every batch variant: the ones it was given, else those of an exact pass down the stack.  What
+        `backward` left (dW, dX, grad) stays as it is."""
+        M = len(self.layers[0].X)
+        if any(len(L.X) != M for L in self.layers):
+            raise ValueError("layers of one stack with different numbers of batch variants")
+        new = lambda *shape, dt=self.dtype: torch.zeros(*shape, dtype=dt, device=self.layers[0].W.device)
+        grads = [[] for _ in self.layers]
+        for v in range(M):
+            dX = None                    # of the layer above, where this one takes it
+            for i, L in enumerate(self.layers):
+                if L.dY:
+                    dY = L.dY[v]
+                elif L.chained:
+                    dY = dX
+                elif L.attention is not None:
+                    dY = self._attention_grad(L, dX, v, new(self.R, L.d_out))
+                elif L.loss is not None:
+                    dY = self._loss_grad(L, v, new(self.R, L.d_out), new(self.R, dt=torch.float32))
+                else:
+                    raise ValueError(f"{L.name}: no gradient to probe it on")
+                grads[i].append(dY)
+                below = self.layers[i + 1] if i + 1 < len(self.layers) else None
+                if below is not None and not below.dY and (below.chained or below.attention is not None):
+                    dX, _ = L.handle.dense_bwd(L.X[v], dY, L.W, H=L.H[v % len(L.H)] if L.H is not None else None)
+        return grads
+
     def probe(self, rho, nu, s: float, seed: int):
         """Alg. 1's probe for every layer (M = number of batch variants).  Returns a [L, 5] device tensor of
-        (V_s, V_act, V_w, p_lo, p_hi).  A chained layer, or one under an attention
-        or a loss, is probed on its own gradient variants."""
+        (V_s, V_act, V_w, p_lo, p_hi).  A layer is probed on its own gradient variants `dY`; where it has none because its gradient comes
+        from the layer above it or from a loss, on the exact gradients of the variants."""
         dev = self.layers[0].W.device
         out = torch.zeros(len(self.layers), 5, dtype=torch.float32, device=dev)
+        grads = [L.dY for L in self.layers] if all(L.dY for L in self.layers) else self._exact_grads()
         for i, L in enumerate(self.layers):
-            L.handle.variance_probe(L.X, L.dY, L.W, float(rho[i]), float(nu[i]), float(s), seed + i, out=out[i])
+            L.handle.variance_probe(L.X, grads[i], L.W, float(rho[i]), float(nu[i]), float(s), seed + i, out=out[i])
         return out
 
     def workspace_bytes(self) -> int:
