@@ -248,10 +248,9 @@ class LinearStack:
         return sum(h.workspace_bytes() for h in self.handles.values())
 
     def device_status(self) -> int:
-        st = 0
-        for h in self.handles.values():
-            st = st or h.device_status()
-        return st
+        """The first status that is not VCAS_OK of the stack's handles, its attentions' and its loss's among them; all are cleared."""
+        ops = list(self.handles.values()) + [o.op for L in self.layers for o in (L.attention, L.loss) if o is not None]
+        return next((st for st in [op.device_status() for op in ops] if st != 0), 0)
 
     def close(self) -> None:
         for h in self.handles.values():

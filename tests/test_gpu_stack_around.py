@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2402_17227_b200 import binding as vb
-from tests.test_gpu_train_step import BF16, F32, make, stack_of
+from tests.test_gpu_train_step import BF16, F32, N, R, VOCAB, make, stack_of
 
 pytestmark = pytest.mark.gpu
 
@@ -58,4 +58,28 @@ def test_a_layer_that_is_given_its_gradients_is_probed_on_them():
     layers[0].loss = None
     with pytest.raises(ValueError):
         st.probe([0.5] * 3, [0.5] * 3, 1.0, seed=1)
+    st.close()
+
+
+def test_status_of_the_loss_and_the_attention_is_the_stacks():
+    layers = make(BF16, seed=6)
+    st = stack_of(layers, BF16)
+    st.backward([1.0] * 3, [1.0] * 3, seed=1)
+    assert st.device_status() == 0
+    layers[0].loss.tokens[0][5] = VOCAB               # outside the vocabulary
+    st.backward([1.0] * 3, [1.0] * 3, seed=1)
+    assert st.device_status() == -1 and st.device_status() == 0
+    layers[0].loss.tokens[0][5] = 0
+    good = layers[2].attention.starts.clone()
+    layers[2].attention.starts[N] = R + 1
+    st.backward([1.0] * 3, [1.0] * 3, seed=1)
+    assert st.device_status() == -1 and st.device_status() == 0
+    # both at once are both cleared
+    layers[0].loss.tokens[0][5] = VOCAB
+    st.backward([1.0] * 3, [1.0] * 3, seed=1)
+    assert st.device_status() == -1 and st.device_status() == 0
+    layers[2].attention.starts.copy_(good)
+    layers[0].loss.tokens[0][5] = 0
+    st.backward([1.0] * 3, [1.0] * 3, seed=1)
+    assert st.device_status() == 0
     st.close()
