@@ -34,7 +34,8 @@ class TokenLossInput:
 @dataclass
 class AttentionInput:
     """An attention between two layers of a stack: q, k and v as the layer under it made them, side by side in [R, heads_q +
-    2 heads_kv, head_dim], and what its forward pass left, one of each per batch variant.  starts: int32 [N + 1], the N data."""
+    2 heads_kv, head_dim], and what its forward pass left, one of each per batch variant.  starts: int32 [N + 1], the N data of T
+    tokens each: 0, T, .., N T."""
     op: vb.Attention
     qkv: list
     o: list
@@ -110,6 +111,8 @@ class LinearStack:
             if L.attention is not None:
                 a = L.attention.op
                 assert layers[i - 1].d_in == a.heads_q * a.head_dim and L.d_out == (a.heads_q + 2 * a.heads_kv) * a.head_dim
+                if L.attention.starts.shape != (N + 1,) or L.attention.starts.tolist() != [n * T for n in range(N + 1)]:
+                    raise ValueError(f"{L.name}: starts of an attention in a stack are those of the {N} data of {T} tokens")
                 L.grad = torch.empty(self.R, L.d_out, dtype=dtype, device=dev)
             if L.loss is not None:
                 assert L.loss.op.vocab <= L.d_out

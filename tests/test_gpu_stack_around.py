@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2402_17227_b200 import binding as vb
-from tests.test_gpu_train_step import BF16, F32, N, R, VOCAB, make, stack_of
+from tests.test_gpu_train_step import BF16, F32, N, R, T, VOCAB, make, stack_of
 
 pytestmark = pytest.mark.gpu
 
@@ -83,3 +83,12 @@ def test_status_of_the_loss_and_the_attention_is_the_stacks():
     st.backward([1.0] * 3, [1.0] * 3, seed=1)
     assert st.device_status() == 0
     st.close()
+
+
+@pytest.mark.parametrize("starts", [range(0, R, T), list(range(0, R + 1, T)) + [R], [0, T + 1] + list(range(2 * T, R + 1, T)),
+                                    list(range(0, R, T)) + [R - 1]])
+def test_starts_that_are_not_those_of_the_data_are_refused(starts):
+    layers = make(BF16, seed=6)
+    layers[2].attention.starts = torch.tensor(list(starts), dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        stack_of(layers, BF16)
