@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass
+from typing import ClassVar
 
 import torch
 
@@ -621,7 +622,9 @@ class TokenLoss(_Handle):
 @dataclass
 class AdamWTensor:
     """One tensor of an AdamW step.  m, v: float32, or float8_e4m3fn (v then holds sqrt(v)) with m_scale and v_scale, one float32
-    for each 256 elements.  copy: bfloat16 copy of p to be written (float32 p)."""
+    for each 256 elements.  copy: bfloat16 copy of p to be written (float32 p).  A field may be set at any time: the next step of every
+    AdamW that has this tensor follows it."""
+    changes: ClassVar[int] = 0       # fields set since their tensors were made, of all tensors
     p: torch.Tensor
     g: torch.Tensor
     m: torch.Tensor
@@ -630,6 +633,16 @@ class AdamWTensor:
     v_scale: torch.Tensor | None = None
     copy: torch.Tensor | None = None
     weight_decay: float = 0.0
+
+    def __post_init__(self):
+        self.__dict__["_version"] = 0
+
+    def __setattr__(self, name, value):
+        d = self.__dict__
+        d[name] = value
+        if "_version" in d:
+            d["_version"] += 1
+            AdamWTensor.changes += 1
 
     @staticmethod
     def make(p, g, bits: int = 32, copy=None, weight_decay: float = 0.0) -> "AdamWTensor":
@@ -643,19 +656,30 @@ class AdamWTensor:
 
 
 class AdamW:
-    """AdamW over a list of tensors in one launch for each combination of types (vcas_adamw_step).  Holds the tensors; `g` of an
-    entry may be set between steps with set_grad."""
+    """AdamW over a list of tensors in one launch for each combination of types (vcas_adamw_step).  Its table of addresses is made once
+    and follows the tensors' fields where these are set.  It holds the memory that the fields had then: a tensor that moves its
+    data by itself (`x.data = ...`) is followed once the field is set again."""
 
     def __init__(self, tensors: list[AdamWTensor]):
         self.device = tensors[0].p.device if tensors else _current_device()
-        self.tensors = list(tensors)
+        self.tensors = tuple(tensors)
         self._table = (AdamWEntry * max(1, len(tensors)))()
         self._args = AdamWArgs()         # filled anew by every step
         self._ref = C.byref(self._args)
+        # of each tensor: the version that the table has, and the memory that it points to
+        self._versions, self._held, self._seen = [None] * len(tensors), [None] * len(tensors), None
+        self._follow()
+
+    def _follow(self) -> None:
+        """Brings the table up to date with the tensors' fields."""
+        seen = AdamWTensor.changes
         for i, t in enumerate(self.tensors):
-            self._fill(i, t)
+            if self._versions[i] != t._version:
+                self._fill(i, t)
+        self._seen = seen
 
     def _fill(self, i: int, t: AdamWTensor) -> None:
+        version = t._version
         bits = 8 if t.m.dtype == torch.float8_e4m3fn else 32
         n = t.p.numel()
         _need(t.p.dtype in _DTYPES, "p is float32 or bfloat16")
@@ -669,26 +693,40 @@ class AdamW:
             _need(scales == [None, None], "float32 states have no scales")
         _need(t.copy is None or (t.copy.dtype == torch.bfloat16 and t.copy.numel() == n and t.p.dtype == torch.float32),
               "copy is bfloat16, of a float32 p")
-        every = [x for x in (t.p, t.m, t.v, t.m_scale, t.v_scale, t.copy) if x is not None]
+        self._check_grad(t, t.g)
+        every = [x for x in (t.g, t.p, t.m, t.v, t.m_scale, t.v_scale, t.copy) if x is not None]
         _need(all(x.is_cuda and x.is_contiguous() for x in every), "device-resident contiguous tensors only")
         _on(self.device, "tensors of a step", *every)
         dp = lambda x: None if x is None else x.data_ptr()
-        self._table[i] = AdamWEntry(dp(t.p), None, dp(t.m), dp(t.v), dp(t.m_scale), dp(t.v_scale), dp(t.copy), n, t.weight_decay,
-                                    _DTYPES[t.p.dtype], 0, bits)
-        self.set_grad(i, t.g)
+        self._table[i] = AdamWEntry(dp(t.p), dp(t.g), dp(t.m), dp(t.v), dp(t.m_scale), dp(t.v_scale), dp(t.copy), n, t.weight_decay,
+                                    _DTYPES[t.p.dtype], _DTYPES[t.g.dtype], bits)
+        self._held[i] = [x.untyped_storage() for x in every]
+        self._versions[i] = version
 
-    def set_grad(self, i: int, g: torch.Tensor) -> None:
-        t = self.tensors[i]
+    def _check_grad(self, t: AdamWTensor, g) -> None:
         _need(g.dtype in _DTYPES and g.numel() == t.p.numel() and g.is_contiguous(), "g is contiguous, float32 or bfloat16, as large as p")
         _on(self.device, "gradients of a step", g)
+
+    def set_grad(self, i: int, g: torch.Tensor) -> None:
+        """The gradient of tensor i: `tensors[i].g = g`, checked at once, and cheaper than the next step's look at all fields."""
+        t = self.tensors[i]
+        self._check_grad(t, g)
+        rest, all_seen = self._versions[i] == t._version, self._seen == AdamWTensor.changes
         t.g = g
-        self._table[i].g, self._table[i].g_dtype = g.data_ptr(), _DTYPES[g.dtype]
+        if rest:                         # the other fields are those of the table
+            self._table[i].g, self._table[i].g_dtype = g.data_ptr(), _DTYPES[g.dtype]
+            self._held[i][0] = g.untyped_storage()
+            self._versions[i] = t._version
+            if all_seen:
+                self._seen = AdamWTensor.changes
 
     def step(self, step: int, *, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, seed: int = 0,
              grad_scale=None, rates=None, seed_dev=None) -> None:
         """step: 1 for the first.  seed: another one each step (8-bit states).  grad_scale: float32 [1] on the device.
         rates (adamw_rates, float32 [3]) and seed_dev (int64 [1]) on the device are read in place of lr and step, and of seed:
         a captured step then follows them."""
+        if self._seen != AdamWTensor.changes:
+            self._follow()
         a = self._args
         a.lr, a.beta1, a.beta2, a.eps, a.step, a.seed = lr, beta1, beta2, eps, step, seed & 0xFFFFFFFFFFFFFFFF
         a.grad_scale = a.rates = a.seed_dev = None
