@@ -91,12 +91,12 @@ __device__ __forceinline__ void product_tiles_ts(uint32_t d, uint32_t a, uint32_
 }
 // D [128 x 64 DC] (+)= A B, A [128 x TN] bf16 in TMEM (each 64 of its columns `gap` TMEM columns behind the 64 before), B a tile of
 // TN rows
-template <int DC, int TN, int K0, int K1>           // columns 16 K0 .. 16 K1 of A
+template <int DC, int TN>
 __device__ __forceinline__ void product_rows(uint32_t d, uint32_t a, int gap, uint32_t b, bool add) {
   constexpr uint32_t idesc = make_idesc(64 * DC, false, true);
   const uint64_t db = desc_rows<TN>(b);
 #pragma unroll
-  for (int k = K0; k < K1; ++k)
+  for (int k = 0; k < TN / 16; ++k)
     umma_bf16_ts(d, a + (uint32_t)((k & 3) * 8 + (k >> 2) * gap), db + (uint64_t)(k * (16 * 128 >> 4)), idesc, add || k != 0 ? 1u : 0u);
 }
 // the rows from `have` on of a tile become 0, by one warp; the products after it see them
@@ -451,8 +451,8 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         if (!ok) break;
         tc_fence_after();
         if (leader) {
-          product_rows<DC, TN, 0, TN / 16>(to, ts + (made & 1) * TN, 0, smem_u32(ring + place * TILE), j != 0);
-          if (j == 0 && few) product_rows<DC, TN, 0, TN / 16>(to, ts + (made & 1) * TN + 32, 0, smem_u32(ring + place * TILE), true);
+          product_rows<DC, TN>(to, ts + (made & 1) * TN, 0, smem_u32(ring + place * TILE), j != 0);
+          if (j == 0 && few) product_rows<DC, TN>(to, ts + (made & 1) * TN + 32, 0, smem_u32(ring + place * TILE), true);
           umma_commit(&s.empty[place]);
           umma_commit(&s.added[h]);
           if (j == tiles - 1) umma_commit(&s.done[h]);
@@ -726,8 +726,8 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         if (!ok) break;
         tc_fence_after();
         if (leader) {
-          product_rows<DC, TN, 0, TN / 16>(tdq, tdp, 64, smem_u32(ring + k_now * TILE), j != 0);
-          if (j == 0 && few) product_rows<DC, TN, 0, TN / 16>(tdq, tdp + 32, 64, smem_u32(ring + k_now * TILE), true);
+          product_rows<DC, TN>(tdq, tdp, 64, smem_u32(ring + k_now * TILE), j != 0);
+          if (j == 0 && few) product_rows<DC, TN>(tdq, tdp + 32, 64, smem_u32(ring + k_now * TILE), true);
           umma_commit(&s.empty[k_now]);
           if (j == tiles - 1) umma_commit(&s.done[0]);
         }
@@ -1009,8 +1009,8 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         tc_fence_after();
         const int q = q_next, g = g_next;
         if (leader) {
-          product_rows<DC, TN, 0, TN / 16>(tdv, ts, 64, smem_u32(ring + g * TILE), i != 0);
-          if (few) product_rows<DC, TN, 0, TN / 16>(tdv, ts + 32, 64, smem_u32(ring + g * TILE), true);
+          product_rows<DC, TN>(tdv, ts, 64, smem_u32(ring + g * TILE), i != 0);
+          if (few) product_rows<DC, TN>(tdv, ts + 32, 64, smem_u32(ring + g * TILE), true);
           umma_commit(&s.empty[g]);
         }
         if (i + 1 < steps) {
@@ -1022,8 +1022,8 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         if (!ok) break;
         tc_fence_after();
         if (leader) {
-          product_rows<DC, TN, 0, TN / 16>(tdk, tdp, 64, smem_u32(ring + q * TILE), i != 0);
-          if (few) product_rows<DC, TN, 0, TN / 16>(tdk, tdp + 32, 64, smem_u32(ring + q * TILE), true);
+          product_rows<DC, TN>(tdk, tdp, 64, smem_u32(ring + q * TILE), i != 0);
+          if (few) product_rows<DC, TN>(tdk, tdp + 32, 64, smem_u32(ring + q * TILE), true);
           umma_commit(&s.empty[q]);
           if (i == steps - 1) umma_commit(&s.done[0]);
         }

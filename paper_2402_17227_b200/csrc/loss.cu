@@ -644,16 +644,16 @@ __global__ void __launch_bounds__(NT) loss_bwd_kernel(BwdParams P) {
 }
 
 // Threads a row: enough for four vectors each.  Slices: while there are fewer rows than CTAs the SMs hold, rows are shared, down to
-// `least` values a slice.
+// 2048 values a slice.
 struct Shape { int threads, slices, per; };
-Shape shape_of(const Loss* l, int rows, int vn, int least) {
+Shape shape_of(const Loss* l, int rows, int vn) {
   const int V = l->desc.vocab, nv = (V + vn - 1) / vn;
   Shape s;
   int slices = 1;
   const int want = 4 * l->num_sms;
   if (rows < want) {
     slices = want / rows;
-    if (slices > (V + least - 1) / least) slices = (V + least - 1) / least;
+    if (slices > (V + 2047) / 2048) slices = (V + 2047) / 2048;
     if (slices > MAX_SLICES) slices = MAX_SLICES;
     if (slices > MAX_UNITS / rows) slices = MAX_UNITS / rows;
     if (slices < 1) slices = 1;
@@ -673,7 +673,7 @@ void launch_fwd(const FwdParams& P, unsigned grid, cudaStream_t st) {
 }
 template <typename T>
 cudaError_t run_fwd(const Loss* l, FwdParams& P, int rows, cudaStream_t st) {
-  Shape s = shape_of(l, rows, Vec<T>::N, 2048);
+  Shape s = shape_of(l, rows, Vec<T>::N);
   if (s.slices > 1 && s.threads == 32) s.threads = 128;      // room for the keys of all slices; a CTA has one row's slice
   P.slices = s.slices; P.per = s.per; P.rows = rows;
   const unsigned grid = (unsigned)rows * s.slices;
@@ -684,7 +684,7 @@ cudaError_t run_fwd(const Loss* l, FwdParams& P, int rows, cudaStream_t st) {
 }
 template <typename T>
 cudaError_t run_bwd(const Loss* l, BwdParams& P, int rows, cudaStream_t st) {
-  const Shape s = shape_of(l, rows, Vec<T>::N, 2048);
+  const Shape s = shape_of(l, rows, Vec<T>::N);
   P.slices = s.slices; P.per = s.per;
   const unsigned grid = (unsigned)rows * s.slices;
   if (s.threads == 32) loss_bwd_kernel<T, 32><<<grid, 32, 0, st>>>(P);
