@@ -36,6 +36,7 @@ extern "C" {
  * reports VCAS_ERR_BAD_ARG.  The results of sequences that such starts make overlap, and of those listed behind them, are unspecified,
  * and rows of sequences that a backward drops may then be left unwritten.
  * A NaN or infinity in a row of q, k or v reaches that sequence's results only.
+ * Beyond 128 sequences the time to find their tiles grows with the square of their number.
  */
 typedef struct vcas_attn_s* vcas_attn;
 

@@ -350,11 +350,13 @@ __device__ __forceinline__ void drain(Shared& s, const Ring& r, int stages, uint
 // scores of each head are in TMEM (64 columns each, beside O's 64 DC), so that a tile's scores are there when the warps come from the
 // one before, and the products of two heads or CTAs fill the tensor pipe.  (Key tiles of 128, one at a time: 1506 of a tile's 3644 cycles
 // went by between the last P and the next scores.)
-// Bound by shared memory: Q is read for each tile of keys (there is no room for it in TMEM), 64-wide products with both operands there
-// take 427 cycles for 256 of arithmetic, and the tiles have to be written too.  Two heads on one copy of K and V save a sixth of
-// that: for heads wider than 64 in groups of an even number (8 x 2048 tokens, 32/8 heads of 128, causal: 282 us by one head, 267
-// by two, both before `few`); narrower ones are bound by their exponentials.  (A part of these as polynomials on the FMA pipe: 298 us for one in eight of
-// the pairs where all by the special function unit took 292; the warps' issue slots were what it cost.)
+// Q is read for each tile of keys (there is no room for it in TMEM): 64-wide products with both operands in shared memory take 427
+// cycles for 256 of arithmetic.  Two heads on one copy of K and V save a sixth of the bytes that the tiles bring in: for heads wider
+// than 64 in groups of an even number (8 x 2048 tokens, 32/8 heads of 128, causal: 282 us by one head, 267 by two, both before `few`);
+// narrower ones are bound by their exponentials.  Over the whole kernel nothing counted is full there: tensor pipe 51 % of the cycles,
+// its reads of shared memory 50 %, special function unit 51 %, issue slots 38 %; the rest goes by in the chain scores -> exponentials -> P ->
+// product of each 64 keys, which two heads fill only in part.  (A part of the exponentials as polynomials on the FMA pipe: 298 us for one in eight
+// of the pairs where all by the special function unit took 292; the warps' issue slots were what it cost.)
 constexpr int FWD_TN = 64;
 template <int DC, int HEADS> constexpr int FWD_STAGES = HEADS == 2 ? 10 : DC == 1 ? 8 : 5;
 template <int HEADS> constexpr int FWD_THREADS = 160 * HEADS + 32;
