@@ -680,6 +680,7 @@ class AdamW:
 
     def _fill(self, i: int, t: AdamWTensor) -> None:
         version = t._version
+        _need(all(x is not None for x in (t.p, t.g, t.m, t.v)), "a tensor of a step has p, g, m and v")
         bits = 8 if t.m.dtype == torch.float8_e4m3fn else 32
         n = t.p.numel()
         _need(t.p.dtype in _DTYPES, "p is float32 or bfloat16")
@@ -704,7 +705,8 @@ class AdamW:
         self._versions[i] = version
 
     def _check_grad(self, t: AdamWTensor, g) -> None:
-        _need(g.dtype in _DTYPES and g.numel() == t.p.numel() and g.is_contiguous(), "g is contiguous, float32 or bfloat16, as large as p")
+        _need(g is not None and g.dtype in _DTYPES and g.numel() == t.p.numel() and g.is_contiguous(),
+              "g is contiguous, float32 or bfloat16, as large as p")
         _on(self.device, "gradients of a step", g)
 
     def set_grad(self, i: int, g: torch.Tensor) -> None:

@@ -103,3 +103,17 @@ def test_memory_that_a_tensor_lets_go_of_stays_the_optimizers():
     e.p = e.p                                         # follows
     opt.step(2, lr=LR)
     assert not torch.equal(e.p, start)
+
+
+@pytest.mark.parametrize("name", ["p", "g", "m", "v"])
+def test_a_field_that_was_taken_away_is_refused(name):
+    e = entry(32)
+    opt = vb.AdamW([e])
+    old = getattr(e, name)
+    setattr(e, name, None)
+    with pytest.raises(ValueError):
+        opt.step(1, lr=LR)
+    with pytest.raises(ValueError):
+        opt.set_grad(0, None)
+    setattr(e, name, old)
+    opt.step(1, lr=LR)
